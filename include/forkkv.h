@@ -422,6 +422,57 @@ fkv_status fkv_produce_tokens_batch(const fkv_produce_seq *seqs, int32_t nseq, c
                                     int64_t rope_max_pos, void *base_kv, void *res_kv, int32_t hkv, int32_t d,
                                     int32_t r, int32_t page_size, void *stream);
 
+/* ------------------------------------------------------------------------ */
+/* 8-bit base cache (device): the base pool in half the bytes.  Block tables,  */
+/* trees, plans, adapters and the residual pool (bf16) stay as they are.       */
+/* ------------------------------------------------------------------------ */
+
+/* A row (K or V of one token and KV head, d = 128 values) is held as 128 e4m3 codes (4 exponent and 3
+ * fraction bits, no infinity) and one exponent byte b, and stands for code * 2^(b - 127).  With amax
+ * the largest magnitude among the row's finite values, E = b - 127 is the smallest integer in [-117, 119] with
+ * amax <= 448 * 2^E; a code is x * 2^-E, clamped to +-448, rounded to nearest even; values that are not
+ * finite become NaN.  Every value the cache stands for is exact in bf16.
+ * base pool  [num_base_pages][fkv_fp8_page_bytes] bytes, 16-byte aligned; a page of 16 tokens holds
+ *              [Hkv][2][2048] codes (K, then V of each head)
+ *                K (token t, dim i): (i/64)*1024 + (t + 16*((i%16)/4))*16 + 8*((i/32)%2) + 4*((i%32)/16) + i%4
+ *                V (token t, dim i): (i/64)*1024 + (i%16 + 16*(t/4))*16 + 8*((i/32)%2) + 4*((i/16)%2) + t%4
+ *              then [Hkv][2][16] exponent bytes (byte t: token t), then padding.  A pool that starts as zeros
+ *              holds zeros. */
+
+/* Bytes of one page, 4096 * hkv and 32 * hkv rounded up to a multiple of 128; 0 unless
+ * page_size = 16, d = 128 and hkv >= 1. */
+int64_t fkv_fp8_page_bytes(int32_t page_size, int32_t hkv, int32_t d);
+
+/* The producer over several sequences (fkv_produce_tokens_batch) into an 8-bit base pool: K (rotated in 64 bits with the
+ * fp32 tables and rounded once; as is without tables) and V are quantised as they are written, C_K and C_V go
+ * into the bf16 residual pool as there.  With rope_cos and every lora_a NULL it writes K and V rows computed
+ * elsewhere.  Slots outside the written ranges keep their bytes.  Same arguments, limits and errors; device
+ * pointers must be aligned to 16 bytes (FKV_ERR_INVALID). */
+fkv_status fkv_produce_tokens_fp8(const fkv_produce_seq *seqs, int32_t nseq, const void *x, int32_t hidden, const void *k_raw,
+                                  const void *v, const float *rope_cos, const float *rope_sin, int64_t rope_max_pos,
+                                  void *base_fp8, void *res_kv, int32_t hkv, int32_t d, int32_t r, int32_t page_size,
+                                  void *stream);
+
+/* One range of a read (a host array of these; bt_base is device memory). */
+typedef struct {
+    const int32_t *bt_base;  /* the sequence's base block-table row */
+    int64_t pos0;            /* first position to read */
+    int64_t n;               /* positions to read (0: nothing to do) */
+    int64_t row0;            /* row of the first one in k_out and v_out */
+} fkv_read_seq;
+
+/* Read back: rows row0 .. row0 + n - 1 of k_out and v_out [rows][hkv][d] bf16 receive, for every sequence, the values
+ * that the cache stands for at positions pos0 .. pos0 + n - 1 (exact; K as written, rotated).  Other rows stay
+ * as they are; ranges may overlap in the cache, not in the rows.  One launch per 32 sequences.  Every sequence is
+ * checked before anything is launched; pointers aligned to 16 bytes. */
+fkv_status fkv_gather_tokens_fp8(const fkv_read_seq *seqs, int32_t nseq, const void *base_fp8, void *k_out, void *v_out, int32_t hkv,
+                                 int32_t d, int32_t page_size, void *stream);
+
+/* fkv_page_copy_list with an 8-bit base pool (copies of FKV_POOL_RES pages go through it as they are).  A copy
+ * of one list may not read a page that another one of it writes. */
+fkv_status fkv_page_copy_list_fp8(const fkv_page_copy *copies, int32_t n, void *base_fp8, void *res_kv, int32_t hkv, int32_t d,
+                                  int32_t r, int32_t page_size, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -138,6 +138,18 @@ class fkv_produce_seq(ctypes.Structure):
 fkv_produce_tokens_batch = _sig("fkv_produce_tokens_batch", c_i32,
                                 [ctypes.POINTER(fkv_produce_seq), c_i32, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_i64,
                                  c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp])
+fkv_fp8_page_bytes = _sig("fkv_fp8_page_bytes", c_i64, [c_i32, c_i32, c_i32])
+fkv_produce_tokens_fp8 = _sig("fkv_produce_tokens_fp8", c_i32, fkv_produce_tokens_batch.argtypes)
+
+
+class fkv_read_seq(ctypes.Structure):
+    _fields_ = [("bt_base", c_vp), ("pos0", c_i64), ("n", c_i64), ("row0", c_i64)]
+
+
+fkv_gather_tokens_fp8 = _sig("fkv_gather_tokens_fp8", c_i32,
+                             [ctypes.POINTER(fkv_read_seq), c_i32, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_vp])
+fkv_page_copy_list_fp8 = _sig("fkv_page_copy_list_fp8", c_i32,
+                              [c_vp, c_i32, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp])
 
 
 def check(status: int, what: str = "") -> None:

@@ -17,6 +17,7 @@
 #include <algorithm>
 #include <string>
 
+#include "fp8_cache.hpp"
 #include "internal.hpp"
 #include "mfma.hpp"
 
@@ -371,8 +372,106 @@ __device__ __forceinline__ void store_shrink(const fkvk::f32x4 &c, int t, uint16
     }
 }
 
-// PAGES: pages per shrink workgroup, one or kShrinkPages.  What is written does not depend on it, to the bit.
-template <int R, int PAGES>
+// Base rows of one page and up to kProdHeads KV heads in the 8-bit format: wave w of the workgroup takes slots
+// 4w .. 4w + 3 of every head.  A lane holds dims 4c .. 4c + 3 of a token and their rotate-half partners 64
+// further, so that the rotation needs no other lane, the largest magnitude of a row is found among 16 lanes,
+// K leaves as whole words and V after a 4x4 byte transpose inside the wave: no LDS, no barrier.  The rotation
+// is computed in 64 bits (products of a bf16 and an fp32 number are exact there) and rounded once, to the code:
+// in 32 bits a value next to the border of two codes could take the wrong one, a step of up to 2^-3 of it.
+// Bound by HBM (the 64-bit work is 8 products of a lane and row).
+__device__ __forceinline__ void produce_base_fp8(const ProduceArgs &a, const ProduceSeq &q, int64_t pp, int h0, int nh) {
+    constexpr int PS = 16, D = 128, HALF = D / 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int k = lane >> 4, c = lane & 15, t = 4 * wave + k;
+    const int64_t tj0 = pp * PS - q.pos0, tj = tj0 + t;  // call indices of slot 0 and of the lane's token
+    const bool ok = tj >= 0 && tj < q.n;
+    const int64_t tf = tj0 + 4 * wave;
+    const bool whole = tf >= 0 && tf + 3 < q.n;  // the wave's four tokens are all written
+    if (tf + 3 < 0 || tf >= q.n) return;
+    unsigned char *pg = reinterpret_cast<unsigned char *>(a.base_kv) + (int64_t)q.bt_base[pp] * fkvk::f8_page_bytes(a.hkv);
+    fkvk::u32x2 raw[kProdHeads][4];  // K, K + 64, V, V + 64
+#pragma unroll
+    for (int i = 0; i < kProdHeads; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) raw[i][j] = fkvk::u32x2{0, 0};
+        if (ok && i < nh) {
+            const int64_t src = ((q.row0 + tj) * a.hkv + h0 + i) * D + 4 * c;
+            raw[i][0] = fkvk::ldg64(a.k_raw + src);
+            raw[i][1] = fkvk::ldg64(a.k_raw + src + HALF);
+            raw[i][2] = fkvk::ldg64(a.v + src);
+            raw[i][3] = fkvk::ldg64(a.v + src + HALF);
+        }
+    }
+    fkvk::f32x4 cs = {1, 1, 1, 1}, sn = {0, 0, 0, 0};
+    if (a.rope_cos && ok) {
+        // table order [pos / 16][f / 16][pos % 16 + 16 ((f % 16) / 4)][f % 4], f = 4c + i
+        const int64_t o = pp * (PS * HALF) + (c >> 2) * 256 + (t + 16 * (c & 3)) * 4;
+        cs = *reinterpret_cast<const fkvk::f32x4 *>(a.rope_cos + o);
+        sn = *reinterpret_cast<const fkvk::f32x4 *>(a.rope_sin + o);
+    }
+    auto unpack = [](const fkvk::u32x2 &lo, const fkvk::u32x2 &hi, float (&x)[8]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            x[2 * i] = fkvk::bf16_lo(lo[i]);
+            x[2 * i + 1] = fkvk::bf16_hi(lo[i]);
+            x[4 + 2 * i] = fkvk::bf16_lo(hi[i]);
+            x[4 + 2 * i + 1] = fkvk::bf16_hi(hi[i]);
+        }
+    };
+    auto finite = [](float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; };
+#pragma unroll
+    for (int i = 0; i < kProdHeads; ++i) {
+        if (i >= nh) break;
+        float x[8];
+        bool fine[8];
+        unpack(raw[i][0], raw[i][1], x);
+        if (a.rope_cos) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // a pair with a value that is not finite: both results are not finite
+                fine[e] = fine[e + 4] = finite(x[e]) && finite(x[e + 4]);
+                const double u = x[e], w = x[e + 4], co = cs[e], si = sn[e];
+                x[e] = fkvk::f8_round_to_odd(u * co - w * si);
+                x[e + 4] = fkvk::f8_round_to_odd(w * co + u * si);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) fine[e] = finite(x[e]);
+        }
+        const fkvk::F8Row kr = fkvk::f8_quantise(x, fine);
+        unpack(raw[i][2], raw[i][3], x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) fine[e] = finite(x[e]);
+        const fkvk::F8Row vr = fkvk::f8_quantise(x, fine);
+        const uint32_t v0 = fkvk::f8_transpose(vr.lo, k), v1 = fkvk::f8_transpose(vr.hi, k);
+        unsigned char *blk = pg + (int64_t)(h0 + i) * fkvk::kF8HeadBytes;
+        unsigned char *vb = blk + fkvk::kF8Block + fkvk::f8_v_word(wave, k, c);
+        unsigned char *ex = pg + fkvk::f8_exp_off(a.hkv, h0 + i) + t;
+        if (ok) {
+            *reinterpret_cast<uint32_t *>(blk + fkvk::f8_k_word(t, c)) = kr.lo;
+            *reinterpret_cast<uint32_t *>(blk + fkvk::f8_k_word(t, c) + 1024) = kr.hi;
+            if (c == 0) {
+                ex[0] = (unsigned char)kr.exp;
+                ex[16] = (unsigned char)vr.exp;
+            }
+        }
+        if (whole) {
+            *reinterpret_cast<uint32_t *>(vb) = v0;
+            *reinterpret_cast<uint32_t *>(vb + 1024) = v1;
+        } else {
+            // the group's tokens outside the range keep their bytes
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (tf + j < 0 || tf + j >= q.n) continue;
+                vb[j] = (unsigned char)(v0 >> (8 * j));
+                vb[1024 + j] = (unsigned char)(v1 >> (8 * j));
+            }
+        }
+    }
+}
+
+// F8: the base rows go into 8-bit pages.  PAGES: pages per shrink workgroup, one or kShrinkPages.  What is written does not depend on it, to the bit.
+template <int R, int PAGES, bool F8>
 __global__ __launch_bounds__(256, PAGES > 1 ? 6 : 2) void produce_kernel(ProduceArgs a) {
     constexpr int PS = 16, D = 128, HALF = D / 2;
     const int lane = threadIdx.x & 63;
@@ -556,12 +655,16 @@ __global__ __launch_bounds__(256, PAGES > 1 ? 6 : 2) void produce_kernel(Produce
     }
     // base K (rotated) and V of one page and up to kProdHeads KV heads: every head's token
     // rows are requested before the first one is stored into LDS
-    __shared__ __attribute__((aligned(16))) uint16_t s_k[kProdHeads][PS * D], s_v[kProdHeads][PS * D];  // [slot][dim]
     const int n_hg = (a.hkv + kProdHeads - 1) / kProdHeads;
     const int b = lb;
     const int h0 = (b % n_hg) * kProdHeads;
     const int nh = min(kProdHeads, a.hkv - h0);
     const int64_t pp = page0 + b / n_hg;
+    if constexpr (F8) {
+        produce_base_fp8(a, q, pp, h0, nh);
+        return;
+    }
+    __shared__ __attribute__((aligned(16))) uint16_t s_k[kProdHeads][PS * D], s_v[kProdHeads][PS * D];  // [slot][dim]
     const int64_t tj0 = pp * PS - pos0;  // call index of slot 0 (negative on a first partial page)
     {
         const int t = threadIdx.x >> 4, c = threadIdx.x & 15;
@@ -655,10 +758,99 @@ __global__ __launch_bounds__(256, PAGES > 1 ? 6 : 2) void produce_kernel(Produce
     }
 }
 
-template <int R>
+template <int R, bool F8>
 void launch_produce(const ProduceArgs &a, unsigned blocks, int pages, hipStream_t st) {
-    if (R > 0 && pages > 1) hipLaunchKernelGGL((produce_kernel<R, R == 0 ? 1 : kShrinkPages>), dim3(blocks), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((produce_kernel<R, 1>), dim3(blocks), dim3(256), 0, st, a);
+    if (R > 0 && pages > 1) hipLaunchKernelGGL((produce_kernel<R, R == 0 ? 1 : kShrinkPages, F8>), dim3(blocks), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((produce_kernel<R, 1, F8>), dim3(blocks), dim3(256), 0, st, a);
+}
+
+// Both batched producers: checks, then one launch per 32 sequences.
+template <bool F8>
+fkv_status produce_batch(const char *name, const fkv_produce_seq *seqs, int32_t nseq, const void *x, int32_t hidden, const void *k_raw,
+                         const void *v, const float *rope_cos, const float *rope_sin, int64_t rope_max_pos, void *base_kv,
+                         void *res_kv, int32_t hkv, int32_t d, int32_t r, int32_t page_size, void *stream) {
+    const std::string fn(name);
+    if (nseq < 0 || (nseq > 0 && !seqs) || hkv < 1 || d != 128 || page_size != 16 ||
+        !(r == 0 || r == 8 || r == 16 || r == 32 || r == 64))
+        return fkv::fail(FKV_ERR_INVALID, fn + ": needs d = 128, page_size = 16, r in {0, 8, 16, 32, 64}");
+    if (!base_kv || !k_raw || !v) return fkv::fail(FKV_ERR_INVALID, fn + ": pool, K or V missing");
+    if ((rope_cos == nullptr) != (rope_sin == nullptr))
+        return fkv::fail(FKV_ERR_INVALID, fn + ": RoPE tables come in pairs");
+    if (F8 && (((uintptr_t)k_raw | (uintptr_t)v | (uintptr_t)x | (uintptr_t)rope_cos | (uintptr_t)rope_sin | (uintptr_t)base_kv |
+                (uintptr_t)res_kv) & 15))
+        return fkv::fail(FKV_ERR_INVALID, fn + ": device pointers must be aligned to 16 bytes");
+    // every sequence is checked before anything is launched
+    for (int32_t i = 0; i < nseq; ++i) {
+        const fkv_produce_seq &q = seqs[i];
+        const std::string who = fn + ": sequence " + std::to_string(i) + ": ";
+        if (q.pos0 < 0 || q.n < 0 || q.row0 < 0) return fkv::fail(FKV_ERR_INVALID, who + "negative position, count or row");
+        if (q.n > (int64_t)1 << 24) return fkv::fail(FKV_ERR_INVALID, who + "too many tokens in one call");
+        if (q.n > 0 && !q.bt_base) return fkv::fail(FKV_ERR_INVALID, who + "base table missing");
+        if (rope_cos && q.pos0 + q.n > rope_max_pos) return fkv::fail(FKV_ERR_INVALID, who + "RoPE table too short");
+        if (q.lora_a && r > 0 && q.n > 0) {
+            if (!x || hidden < kProdChunk || hidden % kProdChunk)
+                return fkv::fail(FKV_ERR_INVALID, who + "x and hidden (a multiple of 1024) required with lora_a");
+            if (!q.bt_res || !res_kv) return fkv::fail(FKV_ERR_INVALID, who + "residual table/pool missing");
+            if (F8 && ((uintptr_t)q.lora_a & 15)) return fkv::fail(FKV_ERR_INVALID, who + "lora_a must be aligned to 16 bytes");
+        }
+    }
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t n_hg = (hkv + kProdHeads - 1) / kProdHeads;
+    for (int32_t c0 = 0; c0 < nseq; c0 += kProdMaxSeqs) {
+        ProduceArgs a{};
+        a.hidden = hidden;
+        a.hkv = hkv;
+        a.x = static_cast<const uint16_t *>(x);
+        a.k_raw = static_cast<const uint16_t *>(k_raw);
+        a.v = static_cast<const uint16_t *>(v);
+        a.rope_cos = rope_cos;
+        a.rope_sin = rope_sin;
+        a.base_kv = static_cast<uint16_t *>(base_kv);
+        a.res_kv = static_cast<uint16_t *>(res_kv);
+        auto pages_of = [&](const fkv_produce_seq &q) {  // pages that its range touches
+            return q.n == 0 ? (int64_t)0 : (q.pos0 + q.n - 1) / page_size - q.pos0 / page_size + 1;
+        };
+        const int32_t c1 = std::min(nseq, c0 + kProdMaxSeqs);
+        int64_t longest = 0, total = 0;
+        for (int32_t i = c0; i < c1; ++i) {
+            if (r == 0 || !seqs[i].lora_a) continue;
+            longest = std::max(longest, pages_of(seqs[i]));
+            total += pages_of(seqs[i]);
+        }
+        const int per_wg = one_page_shrink(longest, total, r) ? 1 : kShrinkPages;
+        int64_t n_shrink = 0, n_base = 0;
+        for (int32_t i = c0; i < c1; ++i) {
+            const fkv_produce_seq &q = seqs[i];
+            if (q.n == 0) continue;
+            const int64_t pages = pages_of(q);
+            ProduceSeq &o = a.seq[a.nseq++];
+            o.bt_base = q.bt_base;
+            o.bt_res = q.bt_res;
+            o.lora_a = r > 0 ? static_cast<const uint16_t *>(q.lora_a) : nullptr;
+            o.pos0 = q.pos0;
+            o.row0 = q.row0;
+            o.n = (int32_t)q.n;
+            o.first_shrink = (int32_t)n_shrink;
+            o.first_base = (int32_t)n_base;  // offset by the shrink count below
+            if (o.lora_a) n_shrink += (pages + per_wg - 1) / per_wg;
+            n_base += pages * n_hg;
+        }
+        if (a.nseq == 0) continue;
+        if (n_shrink + n_base > INT32_MAX) return fkv::fail(FKV_ERR_INVALID, fn + ": batch too large");
+        for (int32_t j = 0; j < a.nseq; ++j) a.seq[j].first_base += (int32_t)n_shrink;
+        a.n_shrink_blocks = (int32_t)n_shrink;
+        const unsigned blocks = (unsigned)(n_shrink + n_base);
+        switch (r) {
+        case 0: launch_produce<0, F8>(a, blocks, per_wg, st); break;
+        case 8: launch_produce<8, F8>(a, blocks, per_wg, st); break;
+        case 16: launch_produce<16, F8>(a, blocks, per_wg, st); break;
+        case 32: launch_produce<32, F8>(a, blocks, per_wg, st); break;
+        default: launch_produce<64, F8>(a, blocks, per_wg, st); break;
+        }
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return fkv::fail(FKV_ERR_HIP, fn + ": " + hipGetErrorString(e));
+    }
+    return FKV_OK;
 }
 }  // namespace
 
@@ -741,83 +933,17 @@ fkv_status fkv_produce_tokens_batch(const fkv_produce_seq *seqs, int32_t nseq, c
                                     int64_t rope_max_pos, void *base_kv, void *res_kv, int32_t hkv, int32_t d,
                                     int32_t r, int32_t page_size, void *stream) {
     fkv::clear_error();
-    if (nseq < 0 || (nseq > 0 && !seqs) || hkv < 1 || d != 128 || page_size != 16 ||
-        !(r == 0 || r == 8 || r == 16 || r == 32 || r == 64))
-        return fkv::fail(FKV_ERR_INVALID, "fkv_produce_tokens: needs d = 128, page_size = 16, r in {0, 8, 16, 32, 64}");
-    if (!base_kv || !k_raw || !v) return fkv::fail(FKV_ERR_INVALID, "fkv_produce_tokens: pool, K or V missing");
-    if ((rope_cos == nullptr) != (rope_sin == nullptr))
-        return fkv::fail(FKV_ERR_INVALID, "fkv_produce_tokens: RoPE tables come in pairs");
-    // every sequence is checked before anything is launched
-    for (int32_t i = 0; i < nseq; ++i) {
-        const fkv_produce_seq &q = seqs[i];
-        const std::string who = "fkv_produce_tokens: sequence " + std::to_string(i) + ": ";
-        if (q.pos0 < 0 || q.n < 0 || q.row0 < 0) return fkv::fail(FKV_ERR_INVALID, who + "negative position, count or row");
-        if (q.n > (int64_t)1 << 24) return fkv::fail(FKV_ERR_INVALID, who + "too many tokens in one call");
-        if (q.n > 0 && !q.bt_base) return fkv::fail(FKV_ERR_INVALID, who + "base table missing");
-        if (rope_cos && q.pos0 + q.n > rope_max_pos) return fkv::fail(FKV_ERR_INVALID, who + "RoPE table too short");
-        if (q.lora_a && r > 0 && q.n > 0) {
-            if (!x || hidden < kProdChunk || hidden % kProdChunk)
-                return fkv::fail(FKV_ERR_INVALID, who + "x and hidden (a multiple of 1024) required with lora_a");
-            if (!q.bt_res || !res_kv) return fkv::fail(FKV_ERR_INVALID, who + "residual table/pool missing");
-        }
-    }
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const int64_t n_hg = (hkv + kProdHeads - 1) / kProdHeads;
-    for (int32_t c0 = 0; c0 < nseq; c0 += kProdMaxSeqs) {
-        ProduceArgs a{};
-        a.hidden = hidden;
-        a.hkv = hkv;
-        a.x = static_cast<const uint16_t *>(x);
-        a.k_raw = static_cast<const uint16_t *>(k_raw);
-        a.v = static_cast<const uint16_t *>(v);
-        a.rope_cos = rope_cos;
-        a.rope_sin = rope_sin;
-        a.base_kv = static_cast<uint16_t *>(base_kv);
-        a.res_kv = static_cast<uint16_t *>(res_kv);
-        auto pages_of = [&](const fkv_produce_seq &q) {  // pages that its range touches
-            return q.n == 0 ? (int64_t)0 : (q.pos0 + q.n - 1) / page_size - q.pos0 / page_size + 1;
-        };
-        const int32_t c1 = std::min(nseq, c0 + kProdMaxSeqs);
-        int64_t longest = 0, total = 0;
-        for (int32_t i = c0; i < c1; ++i) {
-            if (r == 0 || !seqs[i].lora_a) continue;
-            longest = std::max(longest, pages_of(seqs[i]));
-            total += pages_of(seqs[i]);
-        }
-        const int per_wg = one_page_shrink(longest, total, r) ? 1 : kShrinkPages;
-        int64_t n_shrink = 0, n_base = 0;
-        for (int32_t i = c0; i < c1; ++i) {
-            const fkv_produce_seq &q = seqs[i];
-            if (q.n == 0) continue;
-            const int64_t pages = pages_of(q);
-            ProduceSeq &o = a.seq[a.nseq++];
-            o.bt_base = q.bt_base;
-            o.bt_res = q.bt_res;
-            o.lora_a = r > 0 ? static_cast<const uint16_t *>(q.lora_a) : nullptr;
-            o.pos0 = q.pos0;
-            o.row0 = q.row0;
-            o.n = (int32_t)q.n;
-            o.first_shrink = (int32_t)n_shrink;
-            o.first_base = (int32_t)n_base;  // offset by the shrink count below
-            if (o.lora_a) n_shrink += (pages + per_wg - 1) / per_wg;
-            n_base += pages * n_hg;
-        }
-        if (a.nseq == 0) continue;
-        if (n_shrink + n_base > INT32_MAX) return fkv::fail(FKV_ERR_INVALID, "fkv_produce_tokens: batch too large");
-        for (int32_t j = 0; j < a.nseq; ++j) a.seq[j].first_base += (int32_t)n_shrink;
-        a.n_shrink_blocks = (int32_t)n_shrink;
-        const unsigned blocks = (unsigned)(n_shrink + n_base);
-        switch (r) {
-        case 0: launch_produce<0>(a, blocks, per_wg, st); break;
-        case 8: launch_produce<8>(a, blocks, per_wg, st); break;
-        case 16: launch_produce<16>(a, blocks, per_wg, st); break;
-        case 32: launch_produce<32>(a, blocks, per_wg, st); break;
-        default: launch_produce<64>(a, blocks, per_wg, st); break;
-        }
-        hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return fkv::fail(FKV_ERR_HIP, std::string("fkv_produce_tokens: ") + hipGetErrorString(e));
-    }
-    return FKV_OK;
+    return produce_batch<false>("fkv_produce_tokens", seqs, nseq, x, hidden, k_raw, v, rope_cos, rope_sin, rope_max_pos, base_kv,
+                                res_kv, hkv, d, r, page_size, stream);
+}
+
+fkv_status fkv_produce_tokens_fp8(const fkv_produce_seq *seqs, int32_t nseq, const void *x, int32_t hidden, const void *k_raw,
+                                  const void *v, const float *rope_cos, const float *rope_sin, int64_t rope_max_pos,
+                                  void *base_fp8, void *res_kv, int32_t hkv, int32_t d, int32_t r, int32_t page_size,
+                                  void *stream) {
+    fkv::clear_error();
+    return produce_batch<true>("fkv_produce_tokens_fp8", seqs, nseq, x, hidden, k_raw, v, rope_cos, rope_sin, rope_max_pos,
+                               base_fp8, res_kv, hkv, d, r, page_size, stream);
 }
 
 fkv_status fkv_produce_tokens(const int32_t *bt_base, const int32_t *bt_res, int64_t pos0, int64_t n, const void *x,

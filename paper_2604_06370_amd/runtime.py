@@ -306,6 +306,110 @@ def produce_tokens_batch(seqs, x: Optional[torch.Tensor], k_raw: torch.Tensor, v
           "fkv_produce_tokens_batch")
 
 
+# ---- 8-bit base cache ----
+
+
+def fp8_page_bytes(page_size: int, hkv: int, d: int) -> int:
+    """Bytes of one page of an 8-bit base pool: the row length of its uint8 tensor."""
+    n = int(N.fkv_fp8_page_bytes(page_size, hkv, d))
+    if n < 1:
+        raise FKVError(N.FKV_ERR_UNSUPPORTED, "fkv_fp8_page_bytes: needs page_size = 16, d = 128 and hkv >= 1")
+    return n
+
+
+def _refuse(who: str, why: str):
+    raise FKVError(N.FKV_ERR_INVALID, f"{who}: {why}")
+
+
+def _device_tensor(who: str, name: str, t, dtype, shape=None):
+    """t as an argument of a device entry point: contiguous, of this type and shape (None: any length), on the current device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != torch.cuda.current_device():
+        _refuse(who, f"{name} must be a tensor on the current GPU")
+    if t.dtype != dtype or not t.is_contiguous():
+        _refuse(who, f"{name} must be contiguous and of type {dtype}")
+    if shape is not None and (t.dim() != len(shape) or any(b is not None and a != b for a, b in zip(t.shape, shape))):
+        _refuse(who, f"{name} has shape {tuple(t.shape)}, needs {shape}")
+
+
+def _fp8_range(who: str, i: int, bt, pos0: int, n: int, row0: int, rows: int, page_size: int):
+    """One sequence of a write or read: its table row covers its positions, its rows are inside the source or output."""
+    if pos0 < 0 or n < 0 or row0 < 0:
+        _refuse(who, f"sequence {i}: negative position, count or row")
+    if n == 0:
+        return
+    _device_tensor(who, f"sequence {i}: block-table row", bt, torch.int32, (None,))
+    if pos0 + n > bt.numel() * page_size:
+        _refuse(who, f"sequence {i}: positions up to {pos0 + n} past its block-table row of {bt.numel()} pages")
+    if row0 + n > rows:
+        _refuse(who, f"sequence {i}: rows {row0} .. {row0 + n} past the {rows} that there are")
+
+
+def produce_tokens_fp8(seqs, x: Optional[torch.Tensor], k_raw: torch.Tensor, v: torch.Tensor, rope: Optional[tuple],
+                       base_fp8: torch.Tensor, res_kv: Optional[torch.Tensor], hkv: int, d: int, r: int, page_size: int,
+                       stream=None) -> None:
+    """fkv_produce_tokens_fp8: as produce_tokens_batch (seqs = [(bt_base_row, bt_res_row, lora_a, pos0, n, row0), ...]) into
+    an 8-bit base pool, a uint8 tensor [pages][fp8_page_bytes].  rope = None and lora_a = None write K and V rows as given."""
+    who = "fkv_produce_tokens_fp8"
+    _device_tensor(who, "base_fp8", base_fp8, torch.uint8, (None, fp8_page_bytes(page_size, hkv, d)))
+    for name, t in (("k_raw", k_raw), ("v", v)):
+        _device_tensor(who, name, t, torch.bfloat16, (k_raw.shape[0], hkv, d))
+    rows, hidden = k_raw.shape[0], 0
+    if x is not None:
+        _device_tensor(who, "x", x, torch.bfloat16, (rows, None))
+        hidden = x.shape[1]
+    if res_kv is not None:
+        _device_tensor(who, "res_kv", res_kv, torch.bfloat16)
+    if rope is not None:
+        for t in rope:
+            _device_tensor(who, "rope", t, torch.float32)
+    p = lambda t: t.data_ptr() if t is not None else None
+    arr = (N.fkv_produce_seq * max(1, len(seqs)))()
+    for i, (btb, btr, a, pos0, n, row0) in enumerate(seqs):
+        _fp8_range(who, i, btb, pos0, n, row0, rows, page_size)
+        if a is not None and r > 0 and n > 0:
+            _device_tensor(who, f"sequence {i}: lora_a", a, torch.bfloat16, (2, r, hidden))
+            _fp8_range(who, i, btr, pos0, n, row0, rows, page_size)
+        arr[i] = N.fkv_produce_seq(p(btb), p(btr), p(a), int(pos0), int(n), int(row0))
+    cos, sin = (rope[0], rope[1]) if rope is not None else (None, None)
+    max_pos = min(cos.numel(), sin.numel()) // (d // 2) if cos is not None else 0
+    check(N.fkv_produce_tokens_fp8(arr, len(seqs), p(x), hidden, p(k_raw), p(v), p(cos), p(sin), max_pos, p(base_fp8), p(res_kv), hkv,
+                                   d, r, page_size, _stream(stream)), who)
+
+
+def gather_tokens_fp8(seqs, base_fp8: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor, hkv: int, d: int, page_size: int,
+                      stream=None) -> None:
+    """fkv_gather_tokens_fp8: seqs = [(bt_base_row, pos0, n, row0), ...]; rows row0 .. row0 + n - 1 of k_out and v_out
+    [rows][hkv][d] bf16 receive the cache's values at positions pos0 .. pos0 + n - 1."""
+    who = "fkv_gather_tokens_fp8"
+    _device_tensor(who, "base_fp8", base_fp8, torch.uint8, (None, fp8_page_bytes(page_size, hkv, d)))
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        _device_tensor(who, name, t, torch.bfloat16, (k_out.shape[0], hkv, d))
+    arr = (N.fkv_read_seq * max(1, len(seqs)))()
+    for i, (bt, pos0, n, row0) in enumerate(seqs):
+        _fp8_range(who, i, bt, pos0, n, row0, k_out.shape[0], page_size)
+        arr[i] = N.fkv_read_seq(bt.data_ptr() if bt is not None else None, int(pos0), int(n), int(row0))
+    check(N.fkv_gather_tokens_fp8(arr, len(seqs), base_fp8.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), hkv, d, page_size,
+                                  _stream(stream)), who)
+
+
+def page_copy_fp8(copies: Sequence[Tuple[int, int, int, int]], base_fp8: torch.Tensor, res_kv: Optional[torch.Tensor],
+                  hkv: int, d: int, r: int, page_size: int, stream=None) -> None:
+    """fkv_page_copy_list_fp8 for a list of (pool, src, dst, n_valid)."""
+    who = "fkv_page_copy_list_fp8"
+    if not copies:
+        return
+    _device_tensor(who, "base_fp8", base_fp8, torch.uint8, (None, fp8_page_bytes(page_size, hkv, d)))
+    if res_kv is not None:
+        _device_tensor(who, "res_kv", res_kv, torch.bfloat16)
+    pages = (base_fp8.shape[0], res_kv.shape[0] if res_kv is not None else 0)
+    for pool, src, dst, _ in copies:
+        if pool not in (POOL_BASE, POOL_RES) or not (0 <= src < pages[pool] and 0 <= dst < pages[pool]):
+            _refuse(who, f"copy ({pool}, {src}, {dst}) names a page outside its pool")
+    host = np.array(copies, dtype=np.int32).reshape(-1, 4)
+    check(N.fkv_page_copy_list_fp8(host.ctypes.data, len(copies), base_fp8.data_ptr(),
+                                   res_kv.data_ptr() if res_kv is not None else None, hkv, d, r, page_size, _stream(stream)), who)
+
+
 def make_args(*, q, base_kv, res_kv, lora_b, adapter_idx, base_bt, res_bt, seq_lens, out, hq, hkv, d, r,
               page_size, rope=None, plan_dev=None, q_indptr=None, workspace=None, n_q=0, max_q_per_agent=0,
               scale: Optional[float] = None) -> N.fkv_attn_args:
