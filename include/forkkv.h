@@ -473,6 +473,13 @@ fkv_status fkv_gather_tokens_fp8(const fkv_read_seq *seqs, int32_t nseq, const v
 fkv_status fkv_page_copy_list_fp8(const fkv_page_copy *copies, int32_t n, void *base_fp8, void *res_kv, int32_t hkv, int32_t d,
                                   int32_t r, int32_t page_size, void *stream);
 
+/* ResidualAttention over an 8-bit base pool: fkv_residual_attention_decode and _prefill with args->base_kv
+ * pointing to one (16-byte aligned).  The same shapes, plans (a plan serves either format), workspaces, block tables,
+ * residual pool, streams and errors; K_base and V_base are the values the cache stands for, the products take them
+ * exactly (in bf16, as the queries and weights are), sums and softmax statistics are fp32. */
+fkv_status fkv_residual_attention_decode_fp8(const fkv_attn_args *args, const fkv_plan *plan, void *stream);
+fkv_status fkv_residual_attention_prefill_fp8(const fkv_attn_args *args, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -141,6 +141,11 @@ fkv_produce_tokens_batch = _sig("fkv_produce_tokens_batch", c_i32,
 fkv_fp8_page_bytes = _sig("fkv_fp8_page_bytes", c_i64, [c_i32, c_i32, c_i32])
 fkv_produce_tokens_fp8 = _sig("fkv_produce_tokens_fp8", c_i32, fkv_produce_tokens_batch.argtypes)
 
+fkv_residual_attention_decode_fp8 = _sig("fkv_residual_attention_decode_fp8", c_i32,
+                                         [ctypes.POINTER(fkv_attn_args), c_vp, c_vp])
+fkv_residual_attention_prefill_fp8 = _sig("fkv_residual_attention_prefill_fp8", c_i32,
+                                          [ctypes.POINTER(fkv_attn_args), c_vp])
+
 
 class fkv_read_seq(ctypes.Structure):
     _fields_ = [("bt_base", c_vp), ("pos0", c_i64), ("n", c_i64), ("row0", c_i64)]

@@ -46,6 +46,12 @@ __device__ __forceinline__ u32x4 f8_to_bf16x8(uint32_t lo, uint32_t hi, float sc
     return u32x4{a.x, a.y, b.x, b.y};
 }
 
+// The four operands (16x16x32, bf16) of a block's codes as a lane holds them: two 16-byte pieces, two operands each.
+__device__ __forceinline__ void f8_fragments(const u32x4 (&raw)[2], float scale, u32x4 (&out)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = f8_to_bf16x8(raw[i / 2][2 * (i % 2)], raw[i / 2][2 * (i % 2) + 1], scale);
+}
+
 // ---- a wave over four tokens (slots 4 w .. 4 w + 3 of a page) of one head: lane 16 k + c holds dims 4 c .. 4 c + 3
 // (`lo`) and 64 + 4 c .. + 3 (`hi`, their rotate-half partners) of token 4 w + k ----
 

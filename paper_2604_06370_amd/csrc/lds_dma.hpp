@@ -48,6 +48,16 @@ __device__ __forceinline__ void lds_dma16(i32x4 rsrc, int voff, LdsU32x4 *dst) {
     raw_buffer_load_lds(rsrc, reinterpret_cast<__attribute__((address_space(3))) uint32_t *>(dst), 16, voff, 0, 0, POLICY);
 }
 
+// Copy of four bytes per active lane to dst + 4 i.
+__device__ __forceinline__ void lds_dma4(i32x4 rsrc, int voff, LdsU32x4 *dst) {
+    raw_buffer_load_lds(rsrc, reinterpret_cast<__attribute__((address_space(3))) uint32_t *>(dst), 4, voff, 0, 0, 0);
+}
+// Four-byte and one-byte buffer loads into registers.
+__device__ uint32_t raw_buffer_load_b32(i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.i32");
+__device__ uint8_t raw_buffer_load_b8(i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.i8");
+__device__ __forceinline__ uint32_t buf_load4(i32x4 rsrc, int voff) { return raw_buffer_load_b32(rsrc, voff, 0, 0); }
+__device__ __forceinline__ uint32_t buf_load_u8(i32x4 rsrc, int voff) { return raw_buffer_load_b8(rsrc, voff, 0, 0); }
+
 // LDS byte address of an LDS location.
 __device__ __forceinline__ uint32_t lds_addr(const LdsU32x4 *p) {
     return (uint32_t)reinterpret_cast<uintptr_t>(p);
@@ -89,6 +99,49 @@ __device__ __forceinline__ void lds_read8(uint32_t addr0, uint32_t addr1, u32x4 
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(o0[0]), "=&v"(o0[1]), "=&v"(o0[2]), "=&v"(o0[3]), "=&v"(o1[0]), "=&v"(o1[1]), "=&v"(o1[2]), "=&v"(o1[3])
         : "v"(addr0), "v"(addr1)
+        : "memory");
+}
+
+// Two pairs of 16-byte LDS reads: addr0 and addr1, each + 0/1 KB.
+__device__ __forceinline__ void lds_read2x2(uint32_t addr0, uint32_t addr1, u32x4 (&out)[4]) {
+    asm volatile(
+        "ds_read_b128 %0, %4\n\t"
+        "ds_read_b128 %1, %4 offset:1024\n\t"
+        "ds_read_b128 %2, %5\n\t"
+        "ds_read_b128 %3, %5 offset:1024\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(out[0]), "=&v"(out[1]), "=&v"(out[2]), "=&v"(out[3])
+        : "v"(addr0), "v"(addr1)
+        : "memory");
+}
+// An 8-bit K block (two 16-byte pieces at addr, 1 KB apart) with the exponent byte at ke_addr and the word at ve_addr.
+__device__ __forceinline__ void lds_read_f8(uint32_t addr, uint32_t ke_addr, uint32_t ve_addr, u32x4 (&raw)[2], uint32_t &ke,
+                                            uint32_t &ve) {
+    asm volatile(
+        "ds_read_b128 %0, %4\n\t"
+        "ds_read_b128 %1, %4 offset:1024\n\t"
+        "ds_read_u8 %2, %5\n\t"
+        "ds_read_b32 %3, %6\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(raw[0]), "=&v"(raw[1]), "=&v"(ke), "=&v"(ve)
+        : "v"(addr), "v"(ke_addr), "v"(ve_addr)
+        : "memory");
+}
+// The same for two pages: K blocks 4 KB apart, exponent bytes 32 apart.
+__device__ __forceinline__ void lds_read_f8x2(uint32_t addr, uint32_t ke_addr, uint32_t ve_addr, u32x4 (&r0)[2], u32x4 (&r1)[2],
+                                              uint32_t (&ke)[2], uint32_t (&ve)[2]) {
+    asm volatile(
+        "ds_read_b128 %0, %8\n\t"
+        "ds_read_b128 %1, %8 offset:1024\n\t"
+        "ds_read_b128 %2, %8 offset:4096\n\t"
+        "ds_read_b128 %3, %8 offset:5120\n\t"
+        "ds_read_u8 %4, %9\n\t"
+        "ds_read_u8 %5, %9 offset:32\n\t"
+        "ds_read_b32 %6, %10\n\t"
+        "ds_read_b32 %7, %10 offset:32\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r0[0]), "=&v"(r0[1]), "=&v"(r1[0]), "=&v"(r1[1]), "=&v"(ke[0]), "=&v"(ke[1]), "=&v"(ve[0]), "=&v"(ve[1])
+        : "v"(addr), "v"(ke_addr), "v"(ve_addr)
         : "memory");
 }
 

@@ -616,18 +616,21 @@ namespace fkv {
 fkv_status validate_attn_common(const fkv_attn_args *a, const char *who);
 }
 
-extern "C" fkv_status fkv_residual_attention_prefill(const fkv_attn_args *a, void *stream) {
-    fkv::clear_error();
-    fkv_status st = fkv::validate_attn_common(a, "fkv_residual_attention_prefill");
+namespace {
+
+// Both prefill entry points.  fp8: args' base pool holds 8-bit pages.
+fkv_status prefill_impl(const fkv_attn_args *a, void *stream, bool fp8) {
+    const std::string who = fp8 ? "fkv_residual_attention_prefill_fp8" : "fkv_residual_attention_prefill";
+    fkv_status st = fkv::validate_attn_common(a, who.c_str());
     if (st != FKV_OK) return st;
     if (!a->q_indptr || a->n_q < 1)
-        return fkv::fail(FKV_ERR_INVALID, "fkv_residual_attention_prefill: q_indptr and n_q >= 1 are required");
+        return fkv::fail(FKV_ERR_INVALID, who + ": q_indptr and n_q >= 1 are required");
     const int g = a->hq / a->hkv;
     if (g != 4 && g != 8)
-        return fkv::fail(FKV_ERR_UNSUPPORTED, "fkv_residual_attention_prefill: query heads per KV head must be 4 or 8");
+        return fkv::fail(FKV_ERR_UNSUPPORTED, who + ": query heads per KV head must be 4 or 8");
     if (a->rope_cos && (int64_t)a->rope_max_pos < (int64_t)a->max_pages * a->page_size)
         return fkv::fail(FKV_ERR_INVALID,
-                         "fkv_residual_attention_prefill: RoPE table must cover max_pages * page_size positions");
+                         who + ": RoPE table must cover max_pages * page_size positions");
     PrefillArgs pa;
     pa.q = static_cast<const uint16_t *>(a->q);
     pa.base_kv = static_cast<const uint16_t *>(a->base_kv);
@@ -649,17 +652,32 @@ extern "C" fkv_status fkv_residual_attention_prefill(const fkv_attn_args *a, voi
     // query blocks per (agent, KV head); blocks past an agent's own chunk exit at once
     const bool rope = a->rope_cos != nullptr && a->r > 0;
     const int maxq = a->max_q_per_agent > 0 ? a->max_q_per_agent : a->n_q;
-    if (maxq > a->n_q) return fkv::fail(FKV_ERR_INVALID, "fkv_residual_attention_prefill: max_q_per_agent > n_q");
-    const PrefillForm form = prefill_form(a->r, rope, g, (int64_t)a->n_agents * a->hkv, maxq);
+    if (maxq > a->n_q) return fkv::fail(FKV_ERR_INVALID, who + ": max_q_per_agent > n_q");
+    const PrefillForm form = fp8 ? PrefillForm{false, 256} : prefill_form(a->r, rope, g, (int64_t)a->n_agents * a->hkv, maxq);
     pa.blocks_per_agent_head = (int)(((int64_t)maxq * g + 255) / 256) * (256 / form.rows);
     pa.scale_log2 = a->scale * 1.4426950408889634f;
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    hipError_t e = !form.rebuild ? launch_stream(a->r, g, rope, form.rows == 128, pa, hs, a->timing_events)
+    hipError_t e = fp8            ? launch_fp8(a->r, g, pa, hs, a->timing_events)
+                   : !form.rebuild ? launch_stream(a->r, g, rope, form.rows == 128, pa, hs, a->timing_events)
                    : g == 4      ? dispatch_prefill<4>(a->r, pa, hs, a->timing_events)
                                  : dispatch_prefill<8>(a->r, pa, hs, a->timing_events);
     if (e != hipSuccess)
-        return fkv::fail(FKV_ERR_HIP, std::string("fkv_residual_attention_prefill: launch failed: ") + hipGetErrorString(e));
+        return fkv::fail(FKV_ERR_HIP, who + ": launch failed: " + hipGetErrorString(e));
     return FKV_OK;
+}
+
+}  // namespace
+
+extern "C" fkv_status fkv_residual_attention_prefill(const fkv_attn_args *a, void *stream) {
+    fkv::clear_error();
+    return prefill_impl(a, stream, false);
+}
+
+extern "C" fkv_status fkv_residual_attention_prefill_fp8(const fkv_attn_args *a, void *stream) {
+    fkv::clear_error();
+    if (a && ((uintptr_t)a->base_kv & 15))
+        return fkv::fail(FKV_ERR_INVALID, "fkv_residual_attention_prefill_fp8: the base pool must be aligned to 16 bytes");
+    return prefill_impl(a, stream, true);
 }
 
 extern "C" int32_t fkv_prefill_block_rows(int32_t hq, int32_t hkv, int32_t r, int32_t rope, int32_t n_agents, int32_t max_q,

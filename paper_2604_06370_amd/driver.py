@@ -27,8 +27,11 @@ def _bf16(a: np.ndarray, device) -> torch.Tensor:
 class LoadedWorkload:
     def __init__(self, wl: Workload, device="cuda", rope: bool = True, placement_seed: Optional[int] = None,
                  no_residual: bool = False, pages_per_split: int = 0, item_agents: int = 0, base_pages: Optional[int] = None,
-                 res_pages: Optional[int] = None, headroom_pages: int = 16):
+                 res_pages: Optional[int] = None, headroom_pages: int = 16, base_format: str = "bf16"):
+        if base_format not in ("bf16", "fp8"):
+            raise ValueError("base_format must be 'bf16' or 'fp8'")
         self.wl = wl
+        self.fp8 = base_format == "fp8"  # the base pool holds 8-bit pages
         self.device = torch.device(device)
         self.rope = rope and wl.r > 0
         ps, hkv, d, r = wl.page_size, wl.hkv, wl.d, wl.r
@@ -40,7 +43,10 @@ class LoadedWorkload:
         nb = base_pages or need_base
         nr = res_pages or max(need_res + A, 1)
         self.tree = rt.Tree(ps, nb, nr)
-        self.base_kv = torch.zeros((nb, 2, hkv, ps * d), dtype=torch.bfloat16, device=self.device)
+        if self.fp8:
+            self.base_kv = torch.zeros((nb, rt.fp8_page_bytes(ps, hkv, d)), dtype=torch.uint8, device=self.device)
+        else:
+            self.base_kv = torch.zeros((nb, 2, hkv, ps * d), dtype=torch.bfloat16, device=self.device)
         self.res_kv = torch.zeros((nr, max(rt.res_page_elems(ps, r), 1)), dtype=torch.bfloat16, device=self.device)
         # adapters: agent a uses adapter a; agents without residual get -1
         self.lora_b = _bf16(np.stack([wl.b_k, wl.b_v], axis=1), self.device) if r > 0 else None
@@ -73,9 +79,7 @@ class LoadedWorkload:
             btr = torch.from_numpy(bt_r[0]).to(self.device)
             if base_from < p1:
                 rows = torch.from_numpy(wl.base_row[a][base_from:p1]).to(self.device)
-                rt.scatter_tokens(btb, None, base_from, base_k_dev[rows].contiguous(),
-                                  base_v_dev[rows].contiguous(), None, None, self.base_kv, self.res_kv,
-                                  hkv, d, r, ps)
+                self._write_base(btb, base_from, base_k_dev[rows].contiguous(), base_v_dev[rows].contiguous())
             if r > 0 and res_from < p1:
                 ck = _bf16(wl.c_k[a][res_from:p1], self.device)
                 cv = _bf16(wl.c_v[a][res_from:p1], self.device)
@@ -89,7 +93,7 @@ class LoadedWorkload:
             release_some(0, (L0 + ps - 1) // ps + 1)
             release_some(1, (L0 + ps - 1) // ps + 1)
             fp = self.tree.fork(a, a, wl.fork_tokens[a])
-            rt.page_copy(fp.copies, self.base_kv, self.res_kv, hkv, d, r, ps)
+            self._copy_pages(fp.copies)
             fill(a, 0, L0, fp.base_valid, fp.res_valid)
             self.fill_plans.append(fp)
         for a in range(A):
@@ -98,7 +102,7 @@ class LoadedWorkload:
                 release_some(0, len(wl.chunk_tokens[a]) // ps + 2)
                 release_some(1, len(wl.chunk_tokens[a]) // ps + 2)
                 fp = self.tree.cow_append(a, wl.chunk_tokens[a])
-                rt.page_copy(fp.copies, self.base_kv, self.res_kv, hkv, d, r, ps)
+                self._copy_pages(fp.copies)
                 fill(a, L0, fp.seq_len, fp.base_valid, fp.res_valid)
                 self.append_plans.append(fp)
         del base_k_dev, base_v_dev
@@ -109,6 +113,33 @@ class LoadedWorkload:
         self.item_agents = item_agents
         self._decode = None
         self._prefill = None
+
+    # ---- cache writes in the pool's format ----
+    def _copy_pages(self, copies):
+        wl = self.wl
+        copy = rt.page_copy_fp8 if self.fp8 else rt.page_copy
+        copy(copies, self.base_kv, self.res_kv, wl.hkv, wl.d, wl.r, wl.page_size)
+
+    def _write_base(self, bt, pos0, k, v):
+        """K and V rows [n][hkv][d] (K already rotated) at positions pos0 .. of a sequence's base pages."""
+        wl = self.wl
+        if self.fp8:
+            rt.produce_tokens_fp8([(bt, None, None, pos0, k.shape[0], 0)], None, k, v, None, self.base_kv, None, wl.hkv, wl.d,
+                                  wl.r, wl.page_size)
+        else:
+            rt.scatter_tokens(bt, None, pos0, k, v, None, None, self.base_kv, self.res_kv, wl.hkv, wl.d, wl.r, wl.page_size)
+
+    def read_base(self, a: int, pos0: int, n: int):
+        """K and V rows [n][hkv][d] bf16 that agent a's 8-bit base pages hold from position pos0."""
+        if not self.fp8:
+            raise ValueError("read_base: the base pool is not in the 8-bit format")
+        wl = self.wl
+        bt, _, sl = self.tree.block_tables([a], self.max_pages)
+        if pos0 < 0 or n < 0 or pos0 + n > int(sl[0]):
+            raise ValueError(f"read_base: positions {pos0} .. {pos0 + n} of a sequence of {int(sl[0])}")
+        k, v = (torch.empty((n, wl.hkv, wl.d), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        rt.gather_tokens_fp8([(torch.from_numpy(bt[0]).to(self.device), pos0, n, 0)], self.base_kv, k, v, wl.hkv, wl.d, wl.page_size)
+        return k, v
 
     # ---- decode over the agents that have no prefill chunk ----
     def decode_setup(self, agents: Optional[Sequence[int]] = None):
@@ -150,7 +181,8 @@ class LoadedWorkload:
     def decode(self, stream=None) -> torch.Tensor:
         if self._decode is None:
             self.decode_setup()
-        rt.residual_attention_decode(self._decode["args"], self._decode["plan"], stream)
+        call = rt.residual_attention_decode_fp8 if self.fp8 else rt.residual_attention_decode
+        call(self._decode["args"], self._decode["plan"], stream)
         return self._decode["out"]
 
     def append_token(self, a: int, rows: dict) -> rt.FillPlan:
@@ -160,11 +192,10 @@ class LoadedWorkload:
         wl, dev = self.wl, self.device
         ps, hkv, d, r = wl.page_size, wl.hkv, wl.d, wl.r
         fp = self.tree.cow_append(a, [rows["token"]])
-        rt.page_copy(fp.copies, self.base_kv, self.res_kv, hkv, d, r, ps)
+        self._copy_pages(fp.copies)
         bt_b, bt_r, _ = self.tree.block_tables([a], self.max_pages)
         pos = fp.seq_len - 1
-        rt.scatter_tokens(torch.from_numpy(bt_b[0]).to(dev), None, pos, _bf16(rows["k"], dev), _bf16(rows["v"], dev),
-                          None, None, self.base_kv, self.res_kv, hkv, d, r, ps)
+        self._write_base(torch.from_numpy(bt_b[0]).to(dev), pos, _bf16(rows["k"], dev), _bf16(rows["v"], dev))
         if r > 0:
             rt.scatter_tokens(None, torch.from_numpy(bt_r[0]).to(dev), pos, None, None, _bf16(rows["c_k"], dev),
                               _bf16(rows["c_v"], dev), self.base_kv, self.res_kv, hkv, d, r, ps)
@@ -265,7 +296,8 @@ class LoadedWorkload:
     def prefill(self, stream=None) -> torch.Tensor:
         if self._prefill is None:
             self.prefill_setup()
-        rt.residual_attention_prefill(self._prefill["args"], stream)
+        call = rt.residual_attention_prefill_fp8 if self.fp8 else rt.residual_attention_prefill
+        call(self._prefill["args"], stream)
         return self._prefill["out"]
 
     def close(self):

@@ -429,21 +429,55 @@ def make_args(*, q, base_kv, res_kv, lora_b, adapter_idx, base_bt, res_bt, seq_l
     a.n_q = n_q
     a.max_q_per_agent = max_q_per_agent
     a.scale = scale if scale is not None else 1.0 / float(np.sqrt(d))
+    # the binding's own note of the base pool's format: type, shape, whether it is contiguous
+    a.base_pool = (base_kv.dtype, tuple(base_kv.shape), base_kv.is_contiguous()) if base_kv is not None else None
     return a
 
 
+def _pool_format(args: N.fkv_attn_args, fp8: bool, who: str) -> None:
+    """Refuses arguments whose base pool has the other format (its pages have another length)."""
+    pool = getattr(args, "base_pool", None)
+    if pool is None:
+        return
+    dtype, shape, contiguous = pool
+    if not fp8:
+        if dtype == torch.uint8:
+            _refuse(who, "the base pool holds 8-bit pages: use the _fp8 call")
+        return
+    if dtype != torch.uint8:
+        _refuse(who, f"the base pool must be a uint8 tensor of 8-bit pages, not {dtype}")
+    if len(shape) != 2 or not contiguous or shape[1] != N.fkv_fp8_page_bytes(args.page_size, args.hkv, args.d):
+        _refuse(who, f"base pool of shape {shape}: needs contiguous pages of fp8_page_bytes(page_size, hkv, d)")
+
+
 def residual_attention_decode(args: N.fkv_attn_args, plan: DecodePlan, stream=None) -> None:
+    _pool_format(args, False, "fkv_residual_attention_decode")
     check(N.fkv_residual_attention_decode(ctypes.byref(args), plan.handle, _stream(stream)),
           "fkv_residual_attention_decode")
 
 
 def residual_attention_decode_noalloc(args: N.fkv_attn_args, plan: DecodePlan, stream=None) -> None:
     """fkv_residual_attention_decode_noalloc: args.workspace is ignored (static per-GPU array)."""
+    _pool_format(args, False, "fkv_residual_attention_decode_noalloc")
     check(N.fkv_residual_attention_decode_noalloc(ctypes.byref(args), plan.handle, _stream(stream)),
           "fkv_residual_attention_decode_noalloc")
 
 
+def residual_attention_decode_fp8(args: N.fkv_attn_args, plan: DecodePlan, stream=None) -> None:
+    """fkv_residual_attention_decode_fp8: base_kv of the arguments is an 8-bit pool; plans serve both formats."""
+    _pool_format(args, True, "fkv_residual_attention_decode_fp8")
+    check(N.fkv_residual_attention_decode_fp8(ctypes.byref(args), plan.handle, _stream(stream)),
+          "fkv_residual_attention_decode_fp8")
+
+
+def residual_attention_prefill_fp8(args: N.fkv_attn_args, stream=None) -> None:
+    """fkv_residual_attention_prefill_fp8: base_kv of the arguments is an 8-bit pool."""
+    _pool_format(args, True, "fkv_residual_attention_prefill_fp8")
+    check(N.fkv_residual_attention_prefill_fp8(ctypes.byref(args), _stream(stream)), "fkv_residual_attention_prefill_fp8")
+
+
 def residual_attention_prefill(args: N.fkv_attn_args, stream=None) -> None:
+    _pool_format(args, False, "fkv_residual_attention_prefill")
     check(N.fkv_residual_attention_prefill(ctypes.byref(args), _stream(stream)), "fkv_residual_attention_prefill")
 
 

@@ -135,3 +135,46 @@ def test_host_tensors_are_refused(monkeypatch):
         rt.gather_tokens_fp8([(bt, 0, 4, 0)], pool, k, k, 2, 128, 16)
     with pytest.raises(rt.FKVError, match="current GPU"):
         rt.page_copy_fp8([(0, 0, 1, 4)], pool, None, 2, 128, 0, 16)
+
+
+def _attn(**kw):
+    a = N.fkv_attn_args()
+    for name in ("q", "base_kv", "res_kv", "lora_b", "adapter_idx", "base_bt", "res_bt", "seq_lens", "out", "q_indptr", "plan", "workspace"):
+        setattr(a, name, 4096)
+    a.n_agents, a.hq, a.hkv, a.d, a.r, a.page_size, a.max_pages, a.n_q, a.scale, a.workspace_bytes = 2, 8, 2, 128, 16, 16, 4, 5, 0.1, 1 << 20
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("kw", [dict(base_kv=4104), dict(base_kv=None), dict(d=64), dict(page_size=32), dict(r=24), dict(hq=6), dict(hq=2), dict(q=None),
+                                dict(seq_lens=None), dict(scale=-1.0), dict(n_agents=0), dict(rope_cos=4096), dict(lora_b=None)])
+def test_attention_refusals_without_a_gpu(kw):
+    bt = np.zeros((2, 4), np.int32)
+    plan = rt.DecodePlan(bt, np.array([20, 30], np.int32), 8, 2, 16, r=16)
+    for st, name in ((N.fkv_residual_attention_prefill_fp8(ctypes.byref(_attn(**kw)), None), "prefill"),
+                     (N.fkv_residual_attention_decode_fp8(ctypes.byref(_attn(**kw)), plan.handle, None), "decode")):
+        assert st in (N.FKV_ERR_INVALID, N.FKV_ERR_UNSUPPORTED)
+        assert f"fkv_residual_attention_{name}_fp8" in N.fkv_last_error().decode()
+
+
+def test_null_arguments_are_refused():
+    assert N.fkv_residual_attention_prefill_fp8(None, None) == N.FKV_ERR_INVALID
+    assert N.fkv_residual_attention_decode_fp8(None, None, None) == N.FKV_ERR_INVALID
+    assert N.fkv_residual_attention_decode_fp8(ctypes.byref(_attn()), None, None) == N.FKV_ERR_INVALID
+
+
+def test_pool_formats_are_kept_apart():
+    # the binding refuses a pool of the other format before it calls the library
+    args = _attn()
+    args.base_pool = (torch.bfloat16, (4, 2, 2, 2048), True)
+    for call in (rt.residual_attention_prefill_fp8, lambda a: rt.residual_attention_decode_fp8(a, None)):
+        with pytest.raises(rt.FKVError, match="uint8"):
+            call(args)
+    args.base_pool = (torch.uint8, (4, rt.fp8_page_bytes(16, 2, 128)), True)
+    for call in (rt.residual_attention_prefill, lambda a: rt.residual_attention_decode(a, None), lambda a: rt.residual_attention_decode_noalloc(a, None)):
+        with pytest.raises(rt.FKVError, match="8-bit"):
+            call(args)
+    args.base_pool = (torch.uint8, (4, 128), True)
+    with pytest.raises(rt.FKVError, match="fp8_page_bytes"):
+        rt.residual_attention_prefill_fp8(args)
