@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace fkvk {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -36,6 +38,17 @@ __device__ __forceinline__ f32x4 mfma16(const u32x2 &a, const u32x2 &b, const f3
 
 __device__ __forceinline__ f32x16 mfma32x32(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4 mfma32_f16(const u32x4 &a, const u32x4 &b, const f32x4 &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// Two fp32 -> packed fp16 pair (round to nearest even; v_cvt_pk_f16_f32).
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    f16x2 v = {(_Float16)lo, (_Float16)hi};
+    return __builtin_bit_cast(uint32_t, v);
 }
 
 // Two fp32 -> packed bf16 pair (round to nearest even; v_cvt_pk_bf16_f32).
@@ -93,6 +106,18 @@ __device__ __forceinline__ float max_over_groups(float x) {
     const uint32_t v = __float_as_uint(y);
     const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
     return fmaxf(y, __uint_as_float((threadIdx.x & 16) ? b[0] : b[1]));
+}
+
+// Maximum over the 16 lanes of a lane group (row), in every one of them.
+__device__ __forceinline__ float max_over_row(float x) {
+    auto step = [](float y, auto ctrl) __attribute__((always_inline)) {
+        const int v = __float_as_int(y);
+        return fmaxf(y, __int_as_float(__builtin_amdgcn_update_dpp(v, v, decltype(ctrl)::value, 0xf, 0xf, true)));
+    };
+    x = step(x, std::integral_constant<int, 0xB1>{});   // lane ^ 1
+    x = step(x, std::integral_constant<int, 0x4E>{});   // lane ^ 2
+    x = step(x, std::integral_constant<int, 0x141>{});  // the other half of eight lanes
+    return step(x, std::integral_constant<int, 0x140>{});
 }
 
 // Maximum over the two lane halves (lanes l and l^32).

@@ -653,14 +653,18 @@ fkv_status prefill_impl(const fkv_attn_args *a, void *stream, bool fp8) {
     const bool rope = a->rope_cos != nullptr && a->r > 0;
     const int maxq = a->max_q_per_agent > 0 ? a->max_q_per_agent : a->n_q;
     if (maxq > a->n_q) return fkv::fail(FKV_ERR_INVALID, who + ": max_q_per_agent > n_q");
-    const PrefillForm form = fp8 ? PrefillForm{false, 256} : prefill_form(a->r, rope, g, (int64_t)a->n_agents * a->hkv, maxq);
-    pa.blocks_per_agent_head = (int)(((int64_t)maxq * g + 255) / 256) * (256 / form.rows);
     pa.scale_log2 = a->scale * 1.4426950408889634f;
     hipStream_t hs = static_cast<hipStream_t>(stream);
-    hipError_t e = fp8            ? launch_fp8(a->r, g, pa, hs, a->timing_events)
-                   : !form.rebuild ? launch_stream(a->r, g, rope, form.rows == 128, pa, hs, a->timing_events)
-                   : g == 4      ? dispatch_prefill<4>(a->r, pa, hs, a->timing_events)
-                                 : dispatch_prefill<8>(a->r, pa, hs, a->timing_events);
+    hipError_t e;
+    if (fp8) {
+        e = launch_fp8(a->r, g, maxq, pa, hs, a->timing_events);
+    } else {
+        const PrefillForm form = prefill_form(a->r, rope, g, (int64_t)a->n_agents * a->hkv, maxq);
+        pa.blocks_per_agent_head = (int)(((int64_t)maxq * g + 255) / 256) * (256 / form.rows);
+        e = !form.rebuild ? launch_stream(a->r, g, rope, form.rows == 128, pa, hs, a->timing_events)
+            : g == 4      ? dispatch_prefill<4>(a->r, pa, hs, a->timing_events)
+                          : dispatch_prefill<8>(a->r, pa, hs, a->timing_events);
+    }
     if (e != hipSuccess)
         return fkv::fail(FKV_ERR_HIP, who + ": launch failed: " + hipGetErrorString(e));
     return FKV_OK;

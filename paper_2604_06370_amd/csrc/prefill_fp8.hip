@@ -1,13 +1,20 @@
 // ResidualAttention chunked prefill over 8-bit base pages (Section 6 prefill kernel, Algorithm 1 with a block of
 // query rows; fp8_cache.hpp has the page format).
 //
-// One workgroup of eight waves = (agent a, KV head h, block of 256 query rows); its rows are (query token, query
-// head of h), 32 per wave, all of the same agent.  Per 64-key tile (four pages):
-//   staging     wave w takes half w / 4 of page w % 4: its codes come to registers one tile ahead, and leave as bf16 in
-//               the LDS tile that all waves read.  K = K_base + RoPE_p(B_K^T C_K^T) (RoPE on; without tables K_base +
-//               B_K^T C_K^T), V = code * 2^E: a value is converted once per workgroup, not once per wave.
-//   every wave  S^T = K Q^T, causal mask + online softmax, O^T += V^T P^T, acc_r^T += C_V^T P^T  (16x16x32 products)
-// and at the end O = (O + acc_r . B_V[h]) / l (Eq. 4) is written in bf16.
+// One workgroup of eight waves = (agent a, KV head h, block of 32 NRG query rows); its rows are (query token, query head of
+// h), all of the same agent.  Wave w serves row group w % NRG (32 rows) as key group w / NRG.  Per round of eight pages:
+//   staging     wave w takes page w: its codes and rCache rows come to registers one round ahead, and leave as
+//               matrix-core operands in LDS, where all waves read them: a value is converted once per workgroup.
+//               K = K_base + RoPE_p(B_K^T C_K^T) (without tables no rotation), V = code * 2^E.
+//   every wave  S^T = K Q^T, causal mask + online softmax, O^T += V^T P^T, acc_r^T += C_V^T P^T over its 8 NRG / 8 pages
+// and at the end the key groups' rows are merged and O = (O + acc_r . B_V[h]) / l (Eq. 4) is written in bf16.  The launch takes
+// fewer rows per workgroup where 256 leave compute units idle: the rest of a workgroup's waves then share its keys.
+//
+// K and Q are fp16 here, 11 significant bits: the sum of a base key, exact in four bits, and its low-rank part would
+// lose what bf16 keeps of it alone (error of the result 5.6e-3 with bf16 keys at 8B heads, rank 16, over 9000 tokens, 2-norm; 2.2e-3 in
+// fp16).  For their range both are scaled by powers of two: Q by its row's largest magnitude, K by a bound of its page's,
+// max(448 * 2^E over its tokens, the largest |C_K| * sum_rho sqrt(2) max_i |B_K[rho][i]|), so that it stays below 2; both
+// exponents go into the softmax's factor of the page.  V stays bf16, in which it is exact.
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -23,18 +30,22 @@ using namespace fkvk;
 namespace fkvp {
 namespace {
 
-constexpr int D = 128, PS = 16, TILE_KEYS = 64;
-constexpr int WAVES = 8, ROWS_PER_WAVE = 32, ROWS = WAVES * ROWS_PER_WAVE;
+constexpr int D = 128, PS = 16;
+constexpr int WAVES = 8, ROWS_PER_WAVE = 32, ROUND_PAGES = WAVES, ROUND_KEYS = ROUND_PAGES * PS;
 constexpr float kNegInf = -INFINITY, kLazyRescale = 8.f;
 
-template <int R>
+template <int R, int NRG>
 struct Shape {
     static constexpr int RT = R == 0 ? 0 : (R + 15) / 16, RTX = RT > 0 ? RT : 1;
-    // LDS: K tile, V tile ([page][4 KB], fragment order), rCache pages [page][rank tile][1 KB], B_K^T fragments
-    static constexpr int V_OFF = 16384, C_OFF = 32768, B_OFF = C_OFF + RT * 4096;
-    static constexpr int MAIN = B_OFF + RT * 4096;
+    static constexpr int ROWS = NRG * ROWS_PER_WAVE, KG = WAVES / NRG, GP = ROUND_PAGES / KG;  // pages of a key group per round
+    // LDS: K and V ([page][4 KB], fragment order), rCache pages [page][rank tile][1 KB], B_K^T fragments, page exponents
+    static constexpr int V_OFF = ROUND_PAGES * 4096, C_OFF = 2 * V_OFF, B_OFF = C_OFF + RT * ROUND_PAGES * 1024;
+    static constexpr int E_OFF = B_OFF + RT * 4096, MAIN = E_OFF + 64;
     static constexpr int EPI = R * D * 4 + ROWS * (R + 1) * 4;  // B_V and the rank accumulators of the epilogue
-    static constexpr int BYTES = MAIN > EPI ? MAIN : EPI;
+    static constexpr int NF4 = 2 * (8 + RT + 2);                // a wave's rows: oacc, racc, lacc, m
+    static constexpr int MERGE = KG > 1 ? (KG / 2) * NRG * NF4 * 1024 : 0;
+    static constexpr int B2 = MAIN > EPI ? MAIN : EPI;
+    static constexpr int BYTES = B2 > MERGE ? B2 : MERGE;
     static_assert(BYTES <= 160 * 1024, "LDS of one workgroup");
 };
 
@@ -44,10 +55,10 @@ __device__ __forceinline__ u32x2 value_word(uint32_t w, const f32x4 &scale) {
     return u32x2{pack_bf16(lo.x * scale.x, lo.y * scale.y), pack_bf16(hi.x * scale.z, hi.y * scale.w)};
 }
 
-template <int R, int G>
+template <int R, int G, int NRG>
 __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs p) {
-    using S = Shape<R>;
-    constexpr int RT = S::RT, RTX = S::RTX, TPW = ROWS / G;
+    using S = Shape<R, NRG>;
+    constexpr int RT = S::RT, RTX = S::RTX, TPW = S::ROWS / G, GP = S::GP;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[S::BYTES];
     const int hkv = p.hkv, bpa = p.blocks_per_agent_head;
     const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
@@ -64,29 +75,28 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4;
+    const int rg = wave % NRG, kg = wave / NRG;
     const int64_t n = (int64_t)hkv * D;
     const int n_pages = (L + PS - 1) / PS;
     const int last_pos = P0 + (tok_begin + TPW < nq ? tok_begin + TPW : nq) - 1;
-    const int n_tiles = last_pos / TILE_KEYS + 1;
+    const int n_rounds = last_pos / ROUND_KEYS + 1;
     const int32_t *btb = p.base_bt + (int64_t)a * p.max_pages, *btr = R > 0 ? p.res_bt + (int64_t)a * p.max_pages : nullptr;
     const unsigned char *base = reinterpret_cast<const unsigned char *>(p.base_kv);
 
-    // ---- staging: this wave's part of a tile in registers ----
-    // codes of operands (quarters of the head dim) half and half + 2 of page pw: the rotate-half partners
-    const int pw = wave & 3, half = wave >> 2;
-    u32x2 kw[2], vw[2];
+    // ---- staging: this wave's page of a round in registers ----
+    u32x4 kw[2], vw[2];
     uint32_t ke, ve;
     u32x4 c[RTX];
-    f32x4 cs[2], sn[2];
-    auto request = [&](int tile) __attribute__((always_inline)) {
-        const int pg = min(4 * tile + pw, n_pages - 1);  // pages past the sequence repeat its last one; their keys are masked
+    f32x4 cs[4], sn[4];
+    auto request = [&](int round) __attribute__((always_inline)) {
+        const int pg = min(ROUND_PAGES * round + wave, n_pages - 1);  // pages past the sequence repeat its last one; their keys are masked
         const unsigned char *page = base + (int64_t)btb[pg] * f8_page_bytes(hkv);
-        const unsigned char *blk = page + (int64_t)h * kF8HeadBytes + lane * 16 + half * 8;
+        const unsigned char *blk = page + (int64_t)h * kF8HeadBytes + lane * 16;
         const unsigned char *ex = page + f8_exp_off(hkv, h);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            kw[j] = ldg64(blk + 1024 * j);
-            vw[j] = ldg64(blk + kF8Block + 1024 * j);
+            kw[j] = ldg128(blk + 1024 * j);
+            vw[j] = ldg128(blk + kF8Block + 1024 * j);
         }
         ke = ex[col];
         ve = *reinterpret_cast<const uint32_t *>(ex + PS + 4 * grp);
@@ -97,9 +107,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
                 for (int t = 0; t < RT; ++t) c[t] = ldg128(rb + t * 512);
             }
             if (rope) {
-                const int64_t at = (int64_t)pg * (PS * D / 2) + 2 * half * 256 + 4 * lane;  // tiles 2 half, 2 half + 1
+                const int64_t at = (int64_t)pg * (PS * D / 2) + 4 * lane;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
+                for (int j = 0; j < 4; ++j) {
                     cs[j] = *reinterpret_cast<const f32x4 *>(p.rope_cos + at + 256 * j);
                     sn[j] = *reinterpret_cast<const f32x4 *>(p.rope_sin + at + 256 * j);
                 }
@@ -107,91 +117,121 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
         }
     };
     const u32x2 *bkt = reinterpret_cast<const u32x2 *>(lds + S::B_OFF);  // [rank tile][column tile][lane]
-    auto stage = [&](int tile) __attribute__((always_inline)) {
-        const int vis = L - (4 * tile + pw) * PS;  // tokens of the page inside the sequence
+    int *page_exp = reinterpret_cast<int *>(lds + S::E_OFF);
+    float b_sum = 0.f;  // sum over ranks of sqrt(2) max_i |B_K[rho][i]|
+    auto stage = [&](int round) __attribute__((always_inline)) {
+        const int vis = L - (ROUND_PAGES * round + wave) * PS;  // tokens of the page inside the sequence
         if (vis < PS) {  // unwritten values may be any bits, and meet zero weights
-            ve = vis > 4 * grp ? ve : 0u;
             const int left = max(0, min(4, vis - 4 * grp));
             const uint32_t m = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
             ve &= m;
+            ke = col < vis ? ke : 0u;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) vw[j] = u32x2{vw[j].x & m, vw[j].y & m};
+            for (int j = 0; j < 2; ++j) vw[j] = u32x4{vw[j].x & m, vw[j].y & m, vw[j].z & m, vw[j].w & m};
             if constexpr (R > 0) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
                     const u32x2 v = mask4(u32x2{c[t].z, c[t].w}, vis, grp);
-                    c[t].z = v.x;
-                    c[t].w = v.y;
+                    c[t] = col < vis ? u32x4{c[t].x, c[t].y, v.x, v.y} : u32x4{0, 0, v.x, v.y};
                 }
             }
         }
-        unsigned char *kd = lds + pw * 4096 + half * 1024 + lane * 16;
-        const float ks = f8_scale(ke);
+        // the page's exponent: |K| < 2^e
+        float e = (float)((int)ke - 127 + 9);
+        if constexpr (R > 0) {
+            if (use_res) {
+                uint32_t m = 0;  // largest |C_K| of the lane, as two halves
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    if constexpr (R == 8) c[t] = u32x4{grp < 2 ? c[t].x : 0u, grp < 2 ? c[t].y : 0u, c[t].z, c[t].w};  // rank padding
+                    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+                    const u16x2 x = __builtin_bit_cast(u16x2, c[t].x & 0x7fff7fffu), y = __builtin_bit_cast(u16x2, c[t].y & 0x7fff7fffu);
+                    m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_elementwise_max(x, y), __builtin_bit_cast(u16x2, m)));
+                }
+                const uint32_t bits = __float_as_uint(fmaxf(bf16_lo(m), bf16_hi(m)) * b_sum) >> 23;
+                // (a token whose rCache row is not finite has no finite key whatever the exponent)
+                e = fmaxf(e, bits < 255u ? (float)((int)bits - 126) : -200.f);
+            }
+        }
+        const int ep = max(-100, min(126, (int)max_over_groups(max_over_row(e))));
+        if (lane == 0) page_exp[wave] = ep;
+        unsigned char *kd = lds + wave * 4096 + lane * 16;
+        const float ks = __uint_as_float((uint32_t)max(0, min(254, (int)ke - ep)) << 23);
         const f32x4 vs = {f8_scale(ve & 255u), f8_scale((ve >> 8) & 255u), f8_scale((ve >> 16) & 255u), f8_scale(ve >> 24)};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const u32x2 v0 = value_word(vw[j].x, vs), v1 = value_word(vw[j].y, vs);
-            *reinterpret_cast<u32x4 *>(kd + S::V_OFF + 2048 * j) = u32x4{v0.x, v0.y, v1.x, v1.y};
+        for (int q2 = 0; q2 < 4; ++q2) {
+            const u32x2 v0 = value_word(vw[q2 / 2][2 * (q2 % 2)], vs), v1 = value_word(vw[q2 / 2][2 * (q2 % 2) + 1], vs);
+            *reinterpret_cast<u32x4 *>(kd + S::V_OFF + 1024 * q2) = u32x4{v0.x, v0.y, v1.x, v1.y};
         }
+        // K: word w of quarter kk is tile m = 2 kk + w, dims 16 m + 4 grp + 0..3 of token col
+        auto base_key = [&](int m) __attribute__((always_inline)) {
+            const uint32_t x = kw[m / 4][m % 4];
+            const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, ks, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(x, ks, true);
+            return f32x4{lo.x, lo.y, hi.x, hi.y};
+        };
+        auto store_keys = [&](int kk, const f32x4 &x, const f32x4 &y) __attribute__((always_inline)) {
+            *reinterpret_cast<u32x4 *>(kd + 1024 * kk) =
+                u32x4{pack_f16(x.x, x.y), pack_f16(x.z, x.w), pack_f16(y.x, y.y), pack_f16(y.z, y.w)};
+        };
         if (!use_res) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) *reinterpret_cast<u32x4 *>(kd + 2048 * j) = f8_to_bf16x8(kw[j].x, kw[j].y, ks);
+            for (int kk = 0; kk < 4; ++kk) store_keys(kk, base_key(2 * kk), base_key(2 * kk + 1));
             return;
         }
         if constexpr (R > 0) {
-            // U^T tiles 2 half, 2 half + 1 and their partners + 4; lane: dims 16 m + 4 grp + i of token col
-            f32x4 u[4];
+            const float inv = __uint_as_float((uint32_t)(127 - ep) << 23);
+            u32x2 ck[RT];  // C_K * 2^-e
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int m = 2 * half + (j & 1) + 4 * (j >> 1);
-                u[j] = f32x4{0, 0, 0, 0};
+            for (int t = 0; t < RT; ++t)
+                ck[t] = u32x2{pack_bf16(bf16_lo(c[t].x) * inv, bf16_hi(c[t].x) * inv), pack_bf16(bf16_lo(c[t].y) * inv, bf16_hi(c[t].y) * inv)};
+            auto low_rank = [&](int m, f32x4 u) __attribute__((always_inline)) {
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    u32x2 ck = u32x2{c[t].x, c[t].y};
-                    if constexpr (R == 8) ck = grp < 2 ? ck : u32x2{0, 0};  // rank padding
-                    u[j] = mfma16(bkt[(t * 8 + m) * 64 + lane], ck, u[j]);
-                }
-            }
-            if (rope) {
+                for (int t = 0; t < RT; ++t) u = mfma16(bkt[(t * 8 + m) * 64 + lane], ck[t], u);
+                return u;
+            };
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+            for (int kk = 0; kk < 2; ++kk) {  // quarters kk and kk + 2: rotate-half partners
+                f32x4 o[4];
+                if (rope) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float x = u[j][i], y = u[j + 2][i];
-                        u[j][i] = x * cs[j][i] - y * sn[j][i];
-                        u[j + 2][i] = y * cs[j][i] + x * sn[j][i];
+                    for (int w = 0; w < 2; ++w) {
+                        const int m = 2 * kk + w;
+                        const f32x4 x = low_rank(m, f32x4{0, 0, 0, 0}), y = low_rank(m + 4, f32x4{0, 0, 0, 0});
+                        const f32x4 bx = base_key(m), by = base_key(m + 4);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            o[w][i] = __builtin_fmaf(x[i], cs[m][i], __builtin_fmaf(-y[i], sn[m][i], bx[i]));
+                            o[w + 2][i] = __builtin_fmaf(y[i], cs[m][i], __builtin_fmaf(x[i], sn[m][i], by[i]));
+                        }
                     }
-            }
+                } else {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                u32x4 o;
-#pragma unroll
-                for (int w = 0; w < 2; ++w) {  // word w: tile 2 half + w (dims 16 apart)
-                    const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(kw[j][w], ks, false);
-                    const f32x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(kw[j][w], ks, true);
-                    const f32x4 s = f32x4{lo.x, lo.y, hi.x, hi.y} + u[2 * j + w];
-                    const u32x2 pk = pack4(s);
-                    o[2 * w] = pk.x;
-                    o[2 * w + 1] = pk.y;
+                    for (int w = 0; w < 4; ++w) {
+                        const int m = 2 * kk + (w & 1) + 4 * (w >> 1);
+                        o[w] = low_rank(m, base_key(m));
+                    }
                 }
-                *reinterpret_cast<u32x4 *>(kd + 2048 * j) = o;
+                store_keys(kk, o[0], o[1]);
+                store_keys(kk + 2, o[2], o[3]);
             }
-            if (half == 0) {
 #pragma unroll
-                for (int t = 0; t < RT; ++t) *reinterpret_cast<u32x4 *>(lds + S::C_OFF + (pw * RT + t) * 1024 + lane * 16) = c[t];
+            for (int t = 0; t < RT; ++t) {
+                if constexpr (R == 8) c[t] = u32x4{0, 0, col < 8 ? c[t].z : 0u, col < 8 ? c[t].w : 0u};
+                *reinterpret_cast<u32x4 *>(lds + S::C_OFF + (wave * RT + t) * 1024 + lane * 16) = c[t];
             }
         }
     };
 
-    // ---- queries: lane = row, in the contraction order of the stored K operands ----
-    int row_tok[2];
+    // ---- queries: lane = row, in the contraction order of the stored K operands, as fp16 times 2^-eq ----
+    int row_tok[2], eq[2];
     u32x4 qf[2][4];
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
-        const int rr = wave * ROWS_PER_WAVE + nt * 16 + col, tk = tok_begin + rr / G;
+        const int rr = rg * ROWS_PER_WAVE + nt * 16 + col, tk = tok_begin + rr / G;
         const bool ok = tk < nq;
         row_tok[nt] = ok ? tk : -1;
         const uint16_t *qr = p.q + ((int64_t)(q0 + (ok ? tk : 0)) * p.hq + h * G + rr % G) * D;
+        float big = 0.f;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
             u32x4 v = {0, 0, 0, 0};
@@ -199,13 +239,28 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
                 const u32x2 lo = ldg64(qr + 32 * kk + 4 * grp), hi = ldg64(qr + 32 * kk + 16 + 4 * grp);
                 v = u32x4{lo.x, lo.y, hi.x, hi.y};
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) big = fmaxf(big, fmaxf(fabsf(bf16_lo(v[i])), fabsf(bf16_hi(v[i]))));
             qf[nt][kk] = v;
         }
+        eq[nt] = max(-100, min(126, (int)(__float_as_uint(max_over_groups(big)) >> 23) - 126));
+        const float inv = __uint_as_float((uint32_t)(127 - eq[nt]) << 23);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) qf[nt][kk][i] = pack_f16(bf16_lo(qf[nt][kk][i]) * inv, bf16_hi(qf[nt][kk][i]) * inv);
     }
     if constexpr (R > 0) {
         if (use_res) {  // lane (c, g) of fragment (tile t, column tile m): B_K[16t + 4g + 0..3][16m + c]
             u32x2 *dst = reinterpret_cast<u32x2 *>(lds + S::B_OFF);
+            float *part = reinterpret_cast<float *>(lds);  // sums of the waves' ranks
             const uint16_t *bk = p.lora_b + (int64_t)ad * 2 * R * n + (int64_t)h * D;
+            float mine = 0.f;
+            for (int rho = wave; rho < R; rho += WAVES) {
+                const uint32_t w = *reinterpret_cast<const uint32_t *>(bk + (int64_t)rho * n + 2 * lane);
+                mine += max_over_groups(max_over_row(fmaxf(fabsf(bf16_lo(w)), fabsf(bf16_hi(w)))));
+            }
+            if (lane == 0) part[wave] = mine * 1.4143f;
             for (int idx = threadIdx.x; idx < RT * 512; idx += 64 * WAVES) {
                 const int ln = idx & 63, m = (idx >> 6) & 7, t = idx >> 9;
                 uint32_t w[2];
@@ -218,6 +273,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
                 }
                 dst[idx] = u32x2{w[0], w[1]};
             }
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) b_sum += part[w];
         }
     }
 
@@ -230,73 +288,79 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     float m_run[2] = {kNegInf, kNegInf};
     const float cl = p.scale_log2;
     const u32x4 kOnes = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+    constexpr int CP = GP < 4 ? GP : 4;  // pages of one softmax step
 
-    request(0);
-    for (int tile = 0; tile < n_tiles; ++tile) {
-        __syncthreads();  // the last tile is read, the B_K^T fragments are written
-        stage(tile);
-        if (tile + 1 < n_tiles) request(tile + 1);
-        __syncthreads();
-        // ---- scores of the tile's 64 keys, two row tiles ----
-        f32x4 sacc[4][2];
+    // Pages pg0 .. pg0 + CP - 1 of the round in LDS, keys from key0.
+    auto step = [&](int pg0, int key0) __attribute__((always_inline)) {
+        f32x4 sacc[CP][2];
+        int ep[CP];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
+        for (int kt = 0; kt < CP; ++kt) {
+            ep[kt] = page_exp[pg0 + kt];
             sacc[kt][0] = sacc[kt][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
-                const u32x4 kf = *reinterpret_cast<const u32x4 *>(lds + kt * 4096 + kk * 1024 + lane * 16);
-                sacc[kt][0] = mfma32(kf, qf[0][kk], sacc[kt][0]);
-                sacc[kt][1] = mfma32(kf, qf[1][kk], sacc[kt][1]);
+                const u32x4 kf = *reinterpret_cast<const u32x4 *>(lds + (pg0 + kt) * 4096 + kk * 1024 + lane * 16);
+                sacc[kt][0] = mfma32_f16(kf, qf[0][kk], sacc[kt][0]);
+                sacc[kt][1] = mfma32_f16(kf, qf[1][kk], sacc[kt][1]);
             }
         }
-        // ---- causal mask and online softmax (rows in lanes): the maximum moves, and the accumulators are rescaled, only
-        // where a row's scores exceed it by more than 2^kLazyRescale ----
-        const bool full = (tile + 1) * TILE_KEYS - 1 <= P0 + tok_begin;
-        u32x2 pf[4][2];
+        // causal mask and online softmax (rows in lanes): the maximum moves, and the accumulators are rescaled, only
+        // where a row's scores exceed it by more than 2^kLazyRescale
+        const bool full = key0 + CP * PS - 1 <= P0 + tok_begin;
+        u32x2 pf[CP][2];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             if (!full) {
-                const int lim = row_tok[nt] < 0 ? -1 : P0 + row_tok[nt] - tile * TILE_KEYS - 4 * grp;
+                const int lim = row_tok[nt] < 0 ? -1 : P0 + row_tok[nt] - key0 - 4 * grp;
 #pragma unroll
-                for (int kt = 0; kt < 4; ++kt)
+                for (int kt = 0; kt < CP; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sacc[kt][nt][i] = kt * PS + i <= lim ? sacc[kt][nt][i] : kNegInf;
             }
-            float mx = kNegInf;
+            float mx = kNegInf, f[CP];
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
+            for (int kt = 0; kt < CP; ++kt) {
+                f[kt] = fminf(fmaxf(ldexpf(cl, ep[kt] + eq[nt]), 1.2e-38f), 3e38f);  // neither 0 nor infinite: masked scores and zeros stay
+                float x = sacc[kt][nt][0];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sacc[kt][nt][i]);
-            mx = max_over_groups(mx) * cl;
+                for (int i = 1; i < 4; ++i) x = fmaxf(x, sacc[kt][nt][i]);
+                mx = fmaxf(mx, x * f[kt]);
+            }
+            mx = max_over_groups(mx);
             if (__builtin_amdgcn_ballot_w64(mx > m_run[nt] + kLazyRescale) != 0) {
                 const float m_new = fmaxf(m_run[nt], mx);
                 const float alpha = fast_exp2(m_run[nt] - (m_new == kNegInf ? 0.f : m_new));
 #pragma unroll
                 for (int m = 0; m < 8; ++m) oacc[m][nt] *= alpha;
 #pragma unroll
-                for (int t = 0; t < RTX; ++t) racc[t][nt] *= alpha;
+                for (int t = 0; t < RT; ++t) racc[t][nt] *= alpha;
                 lacc[nt] *= alpha;
                 m_run[nt] = m_new;
             }
             const float m_use = m_run[nt] == kNegInf ? 0.f : m_run[nt];
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt) {
+            for (int kt = 0; kt < CP; ++kt) {
                 f32x4 pv;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pv[i] = fast_exp2(__builtin_fmaf(sacc[kt][nt][i], cl, -m_use));
+                for (int i = 0; i < 4; ++i) pv[i] = fast_exp2(__builtin_fmaf(sacc[kt][nt][i], f[kt], -m_use));
                 pf[kt][nt] = pack4(pv);
             }
         }
-        // ---- values, two pages (32 keys) per product; row sums of the weights as the products take them ----
+        // values, two pages (32 keys) per product (one page: its upper half is zero); row sums of the weights as the products take them
+        constexpr bool TWO = CP > 1;
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
+        for (int hf = 0; hf < (TWO ? CP / 2 : 1); ++hf) {
             u32x4 pb[2];
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) pb[nt] = u32x4{pf[2 * hf][nt].x, pf[2 * hf][nt].y, pf[2 * hf + 1][nt].x, pf[2 * hf + 1][nt].y};
-            const unsigned char *vb = lds + S::V_OFF + hf * 8192 + lane * 16;
+            for (int nt = 0; nt < 2; ++nt)
+                pb[nt] = u32x4{pf[TWO ? 2 * hf : 0][nt].x, pf[TWO ? 2 * hf : 0][nt].y, TWO ? pf[TWO ? 2 * hf + 1 : 0][nt].x : 0u,
+                               TWO ? pf[TWO ? 2 * hf + 1 : 0][nt].y : 0u};
+            const unsigned char *vb = lds + S::V_OFF + (pg0 + 2 * hf) * 4096 + lane * 16;
 #pragma unroll
             for (int q2 = 0; q2 < 4; ++q2) {
-                const u32x4 v0 = *reinterpret_cast<const u32x4 *>(vb + q2 * 1024), v1 = *reinterpret_cast<const u32x4 *>(vb + 4096 + q2 * 1024);
+                const u32x4 v0 = *reinterpret_cast<const u32x4 *>(vb + q2 * 1024);
+                const u32x4 v1 = TWO ? *reinterpret_cast<const u32x4 *>(vb + 4096 + q2 * 1024) : u32x4{0, 0, 0, 0};
                 const u32x4 va = {v0.x, v0.y, v1.x, v1.y}, vc = {v0.z, v0.w, v1.z, v1.w};  // dims 32 q2 + col, 32 q2 + 16 + col
 #pragma unroll
                 for (int nt = 0; nt < 2; ++nt) {
@@ -310,12 +374,9 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
                 if (use_res) {
 #pragma unroll
                     for (int t = 0; t < RT; ++t) {
-                        const unsigned char *cb = lds + S::C_OFF + (2 * hf * RT + t) * 1024 + lane * 16 + 8;
-                        u32x2 c0 = *reinterpret_cast<const u32x2 *>(cb), c1 = *reinterpret_cast<const u32x2 *>(cb + RT * 1024);
-                        if constexpr (R == 8) {
-                            c0 = col < 8 ? c0 : u32x2{0, 0};
-                            c1 = col < 8 ? c1 : u32x2{0, 0};
-                        }
+                        const unsigned char *cb = lds + S::C_OFF + ((pg0 + 2 * hf) * RT + t) * 1024 + lane * 16 + 8;
+                        const u32x2 c0 = *reinterpret_cast<const u32x2 *>(cb);
+                        const u32x2 c1 = TWO ? *reinterpret_cast<const u32x2 *>(cb + RT * 1024) : u32x2{0, 0};
                         const u32x4 ca = {c0.x, c0.y, c1.x, c1.y};
 #pragma unroll
                         for (int nt = 0; nt < 2; ++nt) racc[t][nt] = mfma32(ca, pb[nt], racc[t][nt]);
@@ -323,8 +384,55 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
                 }
             }
         }
+    };
+
+    request(0);
+    for (int round = 0; round < n_rounds; ++round) {
+        __syncthreads();  // the last round is read, the B_K^T fragments and rank sums are written (and read)
+        stage(round);
+        if (round + 1 < n_rounds) request(round + 1);
+        __syncthreads();
+#pragma unroll
+        for (int s = 0; s < GP; s += CP) {
+            const int key0 = round * ROUND_KEYS + (kg * GP + s) * PS;
+            if (key0 <= last_pos) step(kg * GP + s, key0);
+        }
     }
     __syncthreads();
+
+    // ---- key groups: the upper half leaves its rows in LDS, the lower half merges them into its own ----
+#pragma unroll
+    for (int half = S::KG / 2; half > 0; half /= 2) {
+        f32x4 *buf = reinterpret_cast<f32x4 *>(lds) + lane;
+        if (kg >= half && kg < 2 * half) {
+            f32x4 *dst = buf + ((kg - half) * NRG + rg) * S::NF4 * 64;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+#pragma unroll
+                for (int m = 0; m < 8; ++m) dst[(nt * (S::NF4 / 2) + m) * 64] = oacc[m][nt];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) dst[(nt * (S::NF4 / 2) + 8 + t) * 64] = racc[t][nt];
+                dst[(nt * (S::NF4 / 2) + 8 + RT) * 64] = f32x4{m_run[nt], lacc[nt][0], 0.f, 0.f};
+            }
+        }
+        __syncthreads();
+        if (kg < half) {
+            const f32x4 *src = buf + (kg * NRG + rg) * S::NF4 * 64;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                const f32x4 ml = src[(nt * (S::NF4 / 2) + 8 + RT) * 64];
+                const float M = fmaxf(m_run[nt], ml.x), Mu = M == kNegInf ? 0.f : M;
+                const float w0 = fast_exp2(m_run[nt] - Mu), w1 = fast_exp2(ml.x - Mu);
+#pragma unroll
+                for (int m = 0; m < 8; ++m) oacc[m][nt] = oacc[m][nt] * w0 + src[(nt * (S::NF4 / 2) + m) * 64] * w1;
+#pragma unroll
+                for (int t = 0; t < RT; ++t) racc[t][nt] = racc[t][nt] * w0 + src[(nt * (S::NF4 / 2) + 8 + t) * 64] * w1;
+                lacc[nt][0] = lacc[nt][0] * w0 + ml.y * w1;
+                m_run[nt] = M;
+            }
+        }
+        __syncthreads();
+    }
 
     // ---- epilogue: O = (acc + acc_r . B_V[h]) / l ----
     if constexpr (R > 0) {
@@ -332,59 +440,85 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
             float *bv = reinterpret_cast<float *>(lds), *acc = bv + R * D;
             const uint16_t *src = p.lora_b + ((int64_t)ad * 2 + 1) * R * n + (int64_t)h * D;
             for (int e = threadIdx.x; e < R * D; e += 64 * WAVES) bv[e] = bf16_to_f32(src[(int64_t)(e / D) * n + e % D]);
+            if (kg == 0) {
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+                for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-                for (int t = 0; t < RT; ++t)
+                    for (int t = 0; t < RT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (16 * t + 4 * grp + i < R) acc[(wave * ROWS_PER_WAVE + nt * 16 + col) * (R + 1) + 16 * t + 4 * grp + i] = racc[t][nt][i];
+                        for (int i = 0; i < 4; ++i)
+                            if (16 * t + 4 * grp + i < R) acc[(rg * ROWS_PER_WAVE + nt * 16 + col) * (R + 1) + 16 * t + 4 * grp + i] = racc[t][nt][i];
+            }
             __syncthreads();
+            if (kg == 0) {
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
+                for (int nt = 0; nt < 2; ++nt)
 #pragma unroll 2
-                for (int rho = 0; rho < R; ++rho) {
-                    const float x = acc[(wave * ROWS_PER_WAVE + nt * 16 + col) * (R + 1) + rho];
+                    for (int rho = 0; rho < R; ++rho) {
+                        const float x = acc[(rg * ROWS_PER_WAVE + nt * 16 + col) * (R + 1) + rho];
 #pragma unroll
-                    for (int m = 0; m < 8; ++m) oacc[m][nt] += x * *reinterpret_cast<const f32x4 *>(bv + rho * D + 16 * m + 4 * grp);
-                }
+                        for (int m = 0; m < 8; ++m) oacc[m][nt] += x * *reinterpret_cast<const f32x4 *>(bv + rho * D + 16 * m + 4 * grp);
+                    }
+            }
         }
     }
+    if (kg > 0) return;
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
         if (row_tok[nt] < 0) continue;
         const float l = lacc[nt][0], inv = l > 0.f ? 1.f / l : 0.f;
-        uint16_t *o = p.out + ((int64_t)(q0 + row_tok[nt]) * p.hq + h * G + (wave * ROWS_PER_WAVE + nt * 16 + col) % G) * D;
+        uint16_t *o = p.out + ((int64_t)(q0 + row_tok[nt]) * p.hq + h * G + (rg * ROWS_PER_WAVE + nt * 16 + col) % G) * D;
 #pragma unroll
         for (int m = 0; m < 8; ++m) *reinterpret_cast<u32x2 *>(o + 16 * m + 4 * grp) = pack4(oacc[m][nt] * inv);
     }
 }
 
-template <int R, int G>
+// Rows per workgroup: the most (of 256, 128, 64, 32) whose workgroups still fill every compute unit of the fullest XCD (an (agent,
+// KV head) pair keeps to one XCD), else 32.
+int rows_of(int64_t pairs, int64_t max_q, int g) {
+    const int64_t per_xcd = (pairs + kXcds - 1) / kXcds;
+    for (int rows = 256; rows > 32; rows /= 2)
+        if (per_xcd * ((max_q * g + rows - 1) / rows) >= kCus / kXcds) return rows;
+    return 32;
+}
+
+template <int R, int G, int NRG>
 hipError_t launch(const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     const int pairs = (pa.n_agents * pa.hkv + kXcds - 1) / kXcds * kXcds;
     // timing events carry the kernel's own start and end timestamps (set by the launch)
     hipEvent_t e0 = ev ? static_cast<hipEvent_t>(ev[0]) : nullptr, e1 = ev ? static_cast<hipEvent_t>(ev[1]) : nullptr;
-    hipExtLaunchKernelGGL((prefill_fp8_kernel<R, G>), dim3(pairs * pa.blocks_per_agent_head), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
+    hipExtLaunchKernelGGL((prefill_fp8_kernel<R, G, NRG>), dim3(pairs * pa.blocks_per_agent_head), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
     return hipGetLastError();
 }
 
+template <int R, int G>
+hipError_t dispatch_rows(int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+    switch (rows) {
+    case 256: return launch<R, G, 8>(pa, st, ev);
+    case 128: return launch<R, G, 4>(pa, st, ev);
+    case 64: return launch<R, G, 2>(pa, st, ev);
+    default: return launch<R, G, 1>(pa, st, ev);
+    }
+}
+
 template <int G>
-hipError_t dispatch(int r, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+hipError_t dispatch(int r, int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     switch (r) {
-    case 0: return launch<0, G>(pa, st, ev);
-    case 8: return launch<8, G>(pa, st, ev);
-    case 16: return launch<16, G>(pa, st, ev);
-    case 32: return launch<32, G>(pa, st, ev);
-    case 64: return launch<64, G>(pa, st, ev);
+    case 0: return dispatch_rows<0, G>(rows, pa, st, ev);
+    case 8: return dispatch_rows<8, G>(rows, pa, st, ev);
+    case 16: return dispatch_rows<16, G>(rows, pa, st, ev);
+    case 32: return dispatch_rows<32, G>(rows, pa, st, ev);
+    case 64: return dispatch_rows<64, G>(rows, pa, st, ev);
     default: return hipErrorInvalidValue;
     }
 }
 
 }  // namespace
 
-hipError_t launch_fp8(int r, int g, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
-    return g == 4 ? dispatch<4>(r, pa, st, ev) : dispatch<8>(r, pa, st, ev);
+hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev) {
+    const int rows = rows_of((int64_t)pa.n_agents * pa.hkv, max_q, g);
+    pa.blocks_per_agent_head = (int)((max_q * g + rows - 1) / rows);
+    return g == 4 ? dispatch<4>(r, rows, pa, st, ev) : dispatch<8>(r, rows, pa, st, ev);
 }
 
 }  // namespace fkvp

@@ -152,8 +152,9 @@ def _attn(**kw):
 def test_attention_refusals_without_a_gpu(kw):
     bt = np.zeros((2, 4), np.int32)
     plan = rt.DecodePlan(bt, np.array([20, 30], np.int32), 8, 2, 16, r=16)
-    for st, name in ((N.fkv_residual_attention_prefill_fp8(ctypes.byref(_attn(**kw)), None), "prefill"),
-                     (N.fkv_residual_attention_decode_fp8(ctypes.byref(_attn(**kw)), plan.handle, None), "decode")):
+    for name in ("prefill", "decode"):
+        call = getattr(N, f"fkv_residual_attention_{name}_fp8")
+        st = call(ctypes.byref(_attn(**kw)), *((plan.handle,) if name == "decode" else ()), None)
         assert st in (N.FKV_ERR_INVALID, N.FKV_ERR_UNSUPPORTED)
         assert f"fkv_residual_attention_{name}_fp8" in N.fkv_last_error().decode()
 
