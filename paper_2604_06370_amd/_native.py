@@ -139,7 +139,7 @@ fkv_produce_tokens_batch = _sig("fkv_produce_tokens_batch", c_i32,
                                 [ctypes.POINTER(fkv_produce_seq), c_i32, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_i64,
                                  c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp])
 fkv_fp8_page_bytes = _sig("fkv_fp8_page_bytes", c_i64, [c_i32, c_i32, c_i32])
-fkv_produce_tokens_fp8 = _sig("fkv_produce_tokens_fp8", c_i32, fkv_produce_tokens_batch.argtypes)
+fkv_produce_tokens_fp8 = _sig("fkv_produce_tokens_fp8", c_i32, [c_vp] + fkv_produce_tokens_batch.argtypes[1:])
 
 fkv_residual_attention_decode_fp8 = _sig("fkv_residual_attention_decode_fp8", c_i32,
                                          [ctypes.POINTER(fkv_attn_args), c_vp, c_vp])
@@ -152,7 +152,7 @@ class fkv_read_seq(ctypes.Structure):
 
 
 fkv_gather_tokens_fp8 = _sig("fkv_gather_tokens_fp8", c_i32,
-                             [ctypes.POINTER(fkv_read_seq), c_i32, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_vp])
+                             [c_vp, c_i32, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_vp])
 fkv_page_copy_list_fp8 = _sig("fkv_page_copy_list_fp8", c_i32,
                               [c_vp, c_i32, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_vp])
 

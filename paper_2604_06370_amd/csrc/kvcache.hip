@@ -471,8 +471,10 @@ __device__ __forceinline__ void produce_base_fp8(const ProduceArgs &a, const Pro
 }
 
 // F8: the base rows go into 8-bit pages.  PAGES: pages per shrink workgroup, one or kShrinkPages.  What is written does not depend on it, to the bit.
+// (Four-page workgroups: the bf16 form's LDS already keeps it to fewer than six waves per SIMD; the 8-bit form, which has less, would
+// spill to reach them: 16 x 2048 tokens at rank 16 362 us, with three waves 146.)
 template <int R, int PAGES, bool F8>
-__global__ __launch_bounds__(256, PAGES > 1 ? 6 : 2) void produce_kernel(ProduceArgs a) {
+__global__ __launch_bounds__(256, PAGES > 1 ? (F8 ? 3 : 6) : 2) void produce_kernel(ProduceArgs a) {
     constexpr int PS = 16, D = 128, HALF = D / 2;
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

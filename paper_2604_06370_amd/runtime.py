@@ -344,6 +344,12 @@ def _fp8_range(who: str, i: int, bt, pos0: int, n: int, row0: int, rows: int, pa
         _refuse(who, f"sequence {i}: rows {row0} .. {row0 + n} past the {rows} that there are")
 
 
+def _table_fits(bt, device: int, end: int, page_size: int) -> bool:
+    """The checks of _fp8_range on a table row, without its messages (calls have tens of sequences, each a microsecond of them)."""
+    return (isinstance(bt, torch.Tensor) and bt.dtype is torch.int32 and bt.get_device() == device and bt.dim() == 1
+            and bt.is_contiguous() and end <= bt.numel() * page_size)
+
+
 def produce_tokens_fp8(seqs, x: Optional[torch.Tensor], k_raw: torch.Tensor, v: torch.Tensor, rope: Optional[tuple],
                        base_fp8: torch.Tensor, res_kv: Optional[torch.Tensor], hkv: int, d: int, r: int, page_size: int,
                        stream=None) -> None:
@@ -363,16 +369,21 @@ def produce_tokens_fp8(seqs, x: Optional[torch.Tensor], k_raw: torch.Tensor, v: 
         for t in rope:
             _device_tensor(who, "rope", t, torch.float32)
     p = lambda t: t.data_ptr() if t is not None else None
-    arr = (N.fkv_produce_seq * max(1, len(seqs)))()
+    device, shrink, items = torch.cuda.current_device(), (2, r, hidden), []
     for i, (btb, btr, a, pos0, n, row0) in enumerate(seqs):
-        _fp8_range(who, i, btb, pos0, n, row0, rows, page_size)
-        if a is not None and r > 0 and n > 0:
-            _device_tensor(who, f"sequence {i}: lora_a", a, torch.bfloat16, (2, r, hidden))
-            _fp8_range(who, i, btr, pos0, n, row0, rows, page_size)
-        arr[i] = N.fkv_produce_seq(p(btb), p(btr), p(a), int(pos0), int(n), int(row0))
+        if not (pos0 >= 0 and n > 0 and row0 >= 0 and row0 + n <= rows and _table_fits(btb, device, pos0 + n, page_size)):
+            _fp8_range(who, i, btb, pos0, n, row0, rows, page_size)
+        with_a = a is not None and r > 0 and n > 0
+        if with_a:
+            if not (a.dtype is torch.bfloat16 and a.get_device() == device and a.shape == shrink and a.is_contiguous()):
+                _device_tensor(who, f"sequence {i}: lora_a", a, torch.bfloat16, shrink)
+            if not _table_fits(btr, device, pos0 + n, page_size):
+                _fp8_range(who, i, btr, pos0, n, row0, rows, page_size)
+        items.append((btb.data_ptr() if n else 0, btr.data_ptr() if with_a else 0, a.data_ptr() if with_a else 0, pos0, n, row0))
+    arr = np.array(items, dtype=np.int64)  # fkv_produce_seq: six 8-byte members
     cos, sin = (rope[0], rope[1]) if rope is not None else (None, None)
     max_pos = min(cos.numel(), sin.numel()) // (d // 2) if cos is not None else 0
-    check(N.fkv_produce_tokens_fp8(arr, len(seqs), p(x), hidden, p(k_raw), p(v), p(cos), p(sin), max_pos, p(base_fp8), p(res_kv), hkv,
+    check(N.fkv_produce_tokens_fp8(arr.ctypes.data, len(seqs), p(x), hidden, p(k_raw), p(v), p(cos), p(sin), max_pos, p(base_fp8), p(res_kv), hkv,
                                    d, r, page_size, _stream(stream)), who)
 
 
@@ -384,11 +395,13 @@ def gather_tokens_fp8(seqs, base_fp8: torch.Tensor, k_out: torch.Tensor, v_out: 
     _device_tensor(who, "base_fp8", base_fp8, torch.uint8, (None, fp8_page_bytes(page_size, hkv, d)))
     for name, t in (("k_out", k_out), ("v_out", v_out)):
         _device_tensor(who, name, t, torch.bfloat16, (k_out.shape[0], hkv, d))
-    arr = (N.fkv_read_seq * max(1, len(seqs)))()
+    device, rows, items = torch.cuda.current_device(), k_out.shape[0], []
     for i, (bt, pos0, n, row0) in enumerate(seqs):
-        _fp8_range(who, i, bt, pos0, n, row0, k_out.shape[0], page_size)
-        arr[i] = N.fkv_read_seq(bt.data_ptr() if bt is not None else None, int(pos0), int(n), int(row0))
-    check(N.fkv_gather_tokens_fp8(arr, len(seqs), base_fp8.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), hkv, d, page_size,
+        if not (pos0 >= 0 and n > 0 and row0 >= 0 and row0 + n <= rows and _table_fits(bt, device, pos0 + n, page_size)):
+            _fp8_range(who, i, bt, pos0, n, row0, rows, page_size)
+        items.append((bt.data_ptr() if n else 0, pos0, n, row0))
+    arr = np.array(items, dtype=np.int64)  # fkv_read_seq: four 8-byte members
+    check(N.fkv_gather_tokens_fp8(arr.ctypes.data, len(seqs), base_fp8.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), hkv, d, page_size,
                                   _stream(stream)), who)
 
 
