@@ -20,7 +20,7 @@ HIPCC = os.path.join(ROCM, "bin", "hipcc")
 ARCH = "gfx950"
 
 HOST_SOURCES = ["tree.cpp", "plan.cpp", "capi.cpp"]
-HIP_SOURCES = ["decode.hip", "decode_fp8.hip", "prefill.hip", "prefill_stream.hip", "prefill_fp8.hip", "kvcache.hip", "kvcache_fp8.hip"]
+HIP_SOURCES = ["decode.hip", "decode_fp8.hip", "prefill.hip", "prefill_stream.hip", "prefill_fp8.hip", "prefill_fp8_stream.hip", "kvcache.hip", "kvcache_fp8.hip"]
 
 HOST_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function"]
 # Packed fp32 VALU instructions are kept out of the device code.

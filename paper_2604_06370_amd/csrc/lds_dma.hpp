@@ -41,6 +41,10 @@ template <int POLICY = kCacheDefault>
 __device__ __forceinline__ u32x4 buf_load16(i32x4 rsrc, int voff) {
     return __builtin_bit_cast(u32x4, raw_buffer_load_b128(rsrc, voff, 0, POLICY));
 }
+// The same at a further uniform offset.
+__device__ __forceinline__ u32x4 buf_load16_at(i32x4 rsrc, int voff, int soff) {
+    return __builtin_bit_cast(u32x4, raw_buffer_load_b128(rsrc, voff, soff, kCacheDefault));
+}
 // Copy: lane i's 16 bytes at byte offset voff of the resource land at dst + 16 i.  The
 // instruction's immediate offset stays 0 (it would shift the LDS destination as well).
 template <int POLICY = kCacheDefault>

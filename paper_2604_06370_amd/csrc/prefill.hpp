@@ -37,7 +37,10 @@ __device__ __forceinline__ void poison_unreached_rows(const PrefillArgs &p, int 
 // Launch of the pipelined kernel (prefill_stream.hip) with 128 or 256 query rows per workgroup.
 hipError_t launch_stream(int r, int g, bool rope, bool rows128, const PrefillArgs &pa, hipStream_t st, void *const *ev);
 
-// Launch of the kernel over 8-bit base pages (prefill_fp8.hip), which sets blocks_per_agent_head for chunks of up to max_q tokens.
+// Launch of the kernels over 8-bit base pages (prefill_fp8.hip), which sets blocks_per_agent_head for chunks of up to max_q tokens.
 hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev);
+
+// The one of large grids (prefill_fp8_stream.hip): 256 query rows per workgroup.
+hipError_t launch_fp8_stream(int r, int g, const PrefillArgs &pa, hipStream_t st, void *const *ev);
 
 }  // namespace fkvp

@@ -518,6 +518,7 @@ hipError_t dispatch(int r, int rows, const PrefillArgs &pa, hipStream_t st, void
 hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev) {
     const int rows = rows_of((int64_t)pa.n_agents * pa.hkv, max_q, g);
     pa.blocks_per_agent_head = (int)((max_q * g + rows - 1) / rows);
+    if (rows == 256) return launch_fp8_stream(r, g, pa, st, ev);
     return g == 4 ? dispatch<4>(r, rows, pa, st, ev) : dispatch<8>(r, rows, pa, st, ev);
 }
 

@@ -1,0 +1,597 @@
+// ResidualAttention chunked prefill over 8-bit base pages, the kernel of large grids (Section 6 prefill kernel, Algorithm 1 with
+// a block of query rows; fp8_cache.hpp has the page format, prefill_fp8.hip the scales of K and Q and the kernel of small grids).
+//
+// One workgroup of four waves = (agent a, KV head h, block of 256 query rows), 64 rows per wave: every operand that a wave
+// reads from LDS serves two 32x32x16 products, so that a 64-key tile costs 128 KB of LDS reads instead of the 256 KB of eight waves of
+// 32 rows, which takes LDS as long as its products take the matrix cores.  One wave per SIMD, up to 512 registers.
+//
+// A wave stages one page per tile (four pages): codes and rCache rows come to registers a tile ahead and leave as operands in
+// LDS, K = K_base + RoPE_p(B_K^T C_K^T) in fp16 times 2^-e, V = code * 2^E in bf16, C_V.  The work goes in steps of 32 keys
+// (half a tile); step i issues, product by product in a written order,
+//   matrix cores   O^T += V^T P^T and acc_r^T += C_V^T P^T of step i - 1, S^T = K Q^T of step i + 1
+//   vector ALU     row maxima and weights of step i, and its share of the staging of the next tile
+// so that a wave has both kinds of work at any time; one barrier per tile.  A change of the running maximum rescales the accumulators at the
+// end of its step, when the products of the step before, which carry the old one, are in.
+#include <hip/hip_ext.h>
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <type_traits>
+#include <utility>
+
+#include "fp8_cache.hpp"
+#include "lds_dma.hpp"
+#include "mfma.hpp"
+#include "prefill.hpp"
+
+using namespace fkvk;
+
+namespace fkvp {
+namespace {
+
+constexpr int D = 128, PS = 16, TILE_KEYS = 64, WAVES = 4, ROWS = 256;
+constexpr float kNegInf = -INFINITY, kLazyRescale = 8.f;
+
+template <int R>
+struct Lay {
+    static constexpr int RT = R == 0 ? 0 : (R + 15) / 16, NRB = (RT + 1) / 2;
+    static constexpr bool LROW = RT == 1;  // rows 16..31 of the rank block are ones: the row sums come with acc_r
+    // K [2 tiles][32-key block][step][lane] 16 B, V [3 tiles][page][32-dim block][lane] 16 B, C_V [3 tiles][page][32-rank block][lane] 16 B
+    static constexpr int V_OFF = 2 * 16384, C_OFF = V_OFF + 3 * 16384, C_TILE = 4 * NRB * 1024;
+    static constexpr int B_OFF = C_OFF + 3 * C_TILE, E_OFF = B_OFF + RT * 4096, MAIN = E_OFF + 64;
+    static constexpr int EPI = R * D * 4 + ROWS * (R + 1) * 4;
+    static constexpr int BYTES = MAIN > EPI ? MAIN : EPI;
+    static_assert(BYTES <= 160 * 1024, "LDS of one workgroup");
+};
+
+typedef __attribute__((address_space(3))) u32x4 *lds128;
+typedef __attribute__((address_space(3))) u32x2 *lds64;
+__device__ __forceinline__ void st128(uint32_t a, const u32x4 &v) { *reinterpret_cast<lds128>((uintptr_t)a) = v; }
+__device__ __forceinline__ void st64(uint32_t a, const u32x2 &v) { *reinterpret_cast<lds64>((uintptr_t)a) = v; }
+__device__ __forceinline__ u32x2 ld64(uint32_t a) { return *reinterpret_cast<const __attribute__((address_space(3))) u32x2 *>((uintptr_t)a); }
+
+// S = A B (FIRST) or S + A B with the scores in vector registers and, BA, the queries in accumulation registers: written as an instruction
+// because the compiler puts the results of all of a kernel's products into one kind of register, and here the 160 to 192 of the
+// outputs belong into accumulation registers while every score is read by vector instructions (a move each).  What the compiler
+// then does not know: two states have to pass between a vector instruction that writes an operand (a copy that the register allocator
+// made, say) and the product, and twelve between the product and a vector instruction that reads its result (score_wait).
+template <bool FIRST, bool BA>
+__device__ __forceinline__ void score_product(f32x16 &s, const u32x4 &a, const u32x4 &b) {
+    if constexpr (FIRST && BA) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b));
+    else if constexpr (FIRST) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+    else if constexpr (BA) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b));
+    else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void score_wait(f32x16 (&s)[2]) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1])); }
+
+// f(integral_constant 0), f(1), ..., f(N - 1): steps whose index selects code, without leaving the unrolling to the optimiser's limits.
+template <int... I, class F>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, F &&f) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F &&f) {
+    each(std::make_integer_sequence<int, N>{}, f);
+}
+__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
+
+template <int R, int G, bool ROPE>
+__device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, int a, int h, int tok_begin) {
+    using S = Lay<R>;
+    constexpr int RT = S::RT, RTX = RT > 0 ? RT : 1, NRB = S::NRB, NRBX = NRB > 0 ? NRB : 1, TPW = ROWS / G;
+    constexpr bool LROW = S::LROW;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int col = lane & 15, grp = lane >> 4, hh = lane >> 5, r32 = lane & 31;
+    const int hkv = p.hkv;
+    const int64_t n = (int64_t)hkv * D;
+    const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
+    const int L = p.seq_lens[a], P0 = L - nq;
+    const int ad = R > 0 ? p.adapter_idx[a] : -1;
+    const int n_pages = (L + PS - 1) / PS;
+    const int last_pos = P0 + (tok_begin + TPW < nq ? tok_begin + TPW : nq) - 1;
+    const int n_tiles = last_pos / TILE_KEYS + 1;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
+    const int32_t *btb = p.base_bt + (int64_t)a * p.max_pages, *btr = R > 0 ? p.res_bt + (int64_t)a * p.max_pages : nullptr;
+    const unsigned char *base = reinterpret_cast<const unsigned char *>(p.base_kv);
+    int *page_exp = reinterpret_cast<int *>(lds + S::E_OFF);  // [2 tiles][page]
+
+    // ---- staging: page `wave` of a tile (pages past the sequence repeat its last one; their keys are masked) ----
+    u32x4 kw[2], vw[2];
+    uint32_t ke, ve;
+    u32x4 c[RTX];
+    f32x4 cs[4], sn[4];
+    auto page_of = [&](int tile) __attribute__((always_inline)) { return min(4 * tile + wave, n_pages - 1); };
+    // (buffer loads: a scalar base and one lane offset; lane addresses of 64 bits would be kept in registers for the launch)
+    const int off16 = lane * 16, off_ve = PS + 4 * grp, off_ke = col;
+    // Page ids of this wave's pages of 64 tiles, one per lane, and of the 64 after them: an id read where it is used would hold up the wave.
+    auto ids = [&](int chunk, int &b, int &r) __attribute__((always_inline)) {
+        const int pg = min((64 * chunk + lane) * 4 + wave, n_pages - 1);
+        b = btb[pg];
+        r = R > 0 ? btr[pg] : 0;
+    };
+    int idb, idr, idb_next, idr_next;
+    ids(0, idb, idr);
+    ids(1, idb_next, idr_next);
+    auto request = [&](int tile) __attribute__((always_inline)) {  // tiles in order, from 0
+        if (tile > 0 && (tile & 63) == 0) {
+            idb = idb_next;
+            idr = idr_next;
+            ids((tile >> 6) + 1, idb_next, idr_next);
+        }
+        const uint64_t page = reinterpret_cast<uint64_t>(base) + (int64_t)__builtin_amdgcn_readlane(idb, tile & 63) * f8_page_bytes(hkv);
+        const i32x4 blk = block_rsrc(page + (int64_t)h * kF8HeadBytes, kF8HeadBytes), ex = block_rsrc(page + f8_exp_off(hkv, h), 2 * PS);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            kw[j] = buf_load16_at(blk, off16, 1024 * j);
+            vw[j] = buf_load16_at(blk, off16, kF8Block + 1024 * j);
+        }
+        ke = buf_load_u8(ex, off_ke);
+        ve = buf_load4(ex, off_ve);
+        if constexpr (R > 0) {
+            const i32x4 rb = block_rsrc(reinterpret_cast<uint64_t>(p.res_kv) + (int64_t)__builtin_amdgcn_readlane(idr, tile & 63) * (RT * 1024), RT * 1024);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) c[t] = buf_load16_at(rb, off16, t * 1024);
+        }
+    };
+    auto request_angles = [&](int tile, int m) __attribute__((always_inline)) {  // of frequency tile m
+        if constexpr (ROPE) {
+            const int64_t at = (int64_t)page_of(tile) * (PS * D / 2 * 4);
+            const i32x4 rc = block_rsrc(reinterpret_cast<uint64_t>(p.rope_cos) + at, PS * D / 2 * 4);
+            const i32x4 rs = block_rsrc(reinterpret_cast<uint64_t>(p.rope_sin) + at, PS * D / 2 * 4);
+            cs[m] = __builtin_bit_cast(f32x4, buf_load16_at(rc, off16, 1024 * m));
+            sn[m] = __builtin_bit_cast(f32x4, buf_load16_at(rs, off16, 1024 * m));
+        }
+    };
+    float b_sum = 0.f;
+    // staging of one page in parts, spread over the 36 slots of a tile's two steps
+    struct Staging {
+        uint32_t kd, vd, cd;
+        float e, ks, inv;
+        int ep;
+        f32x4 vs;
+        u32x2 ck[RTX];
+        f32x4 x, y, bx, by;
+        u32x2 pk[2][2];  // [partner][tile of the quarter], packed
+    };
+    const uint32_t bkt = lds0 + S::B_OFF + lane * 8;  // B_K^T fragments [rank tile][column tile][lane]
+    constexpr int PARTS = 30;
+    auto low_rank = [&](const Staging &g, int m, f32x4 u) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < RT; ++t) u = mfma16(ld64(bkt + (t * 8 + m) * 512), g.ck[t], u);
+        return u;
+    };
+    auto base_key = [&](const Staging &g, int m) __attribute__((always_inline)) {
+        const uint32_t w = kw[m / 4][m % 4];
+        const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, g.ks, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, g.ks, true);
+        return f32x4{lo.x, lo.y, hi.x, hi.y};
+    };
+    auto stage_part = [&](Staging &g, int tile, auto part_tag) __attribute__((always_inline)) {
+        constexpr int part = decltype(part_tag)::value;
+        if constexpr (part >= 5 && part <= 17 && part % 4 == 1) request_angles(tile, (part - 5) / 4);  // nine parts before their use
+        if constexpr (part == 0) {
+            int lane = threadIdx.x & 63;
+            asm("" : "+v"(lane));  // what follows from it is formed here, not kept for the launch
+            const int col = lane & 15, grp = lane >> 4;
+            const int vis = L - (4 * tile + wave) * PS;  // tokens of the page inside the sequence
+            if (vis < PS) {  // unwritten values may be any bits, and meet zero weights
+                const int left = max(0, min(4, vis - 4 * grp));
+                const uint32_t m = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
+                ve &= m;
+                ke = col < vis ? ke : 0u;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) vw[j] = u32x4{vw[j].x & m, vw[j].y & m, vw[j].z & m, vw[j].w & m};
+                if constexpr (R > 0) {
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        const u32x2 v = mask4(u32x2{c[t].z, c[t].w}, vis, grp);
+                        c[t] = col < vis ? u32x4{c[t].x, c[t].y, v.x, v.y} : u32x4{0, 0, v.x, v.y};
+                    }
+                }
+            }
+            // K: operand of step 2 kk + grp / 2, lane half grp % 2, row 16 (page % 2) + col; V, C_V: words of four tokens 4 grp .. + 3,
+            // the lower or upper eight bytes of lane half grp % 2
+            const uint32_t at = ((lane & 16) * 2 + (lane & 15)) * 16;  // of lane half grp % 2, row col
+            g.kd = lds0 + (tile & 1) * 16384 + (wave >> 1) * 8192 + (wave & 1) * 256 + (lane & 32) * 32 + at;
+            g.vd = lds0 + S::V_OFF + (tile % 3) * 16384 + wave * 4096 + (lane & 32) / 4 + at;
+            g.cd = g.vd + (S::C_OFF - S::V_OFF) + (tile % 3) * (S::C_TILE - 16384) + wave * (NRB * 1024 - 4096);
+            g.e = (float)((int)ke - 127 + 9);
+            if constexpr (R > 0) {
+                typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+                u16x2 m = {0, 0};
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    if constexpr (R == 8) c[t] = u32x4{grp < 2 ? c[t].x : 0u, grp < 2 ? c[t].y : 0u, col < 8 ? c[t].z : 0u, col < 8 ? c[t].w : 0u};
+                    const u16x2 x = __builtin_bit_cast(u16x2, c[t].x & 0x7fff7fffu), y = __builtin_bit_cast(u16x2, c[t].y & 0x7fff7fffu);
+                    m = __builtin_elementwise_max(__builtin_elementwise_max(x, y), m);
+                }
+                const uint32_t w = __builtin_bit_cast(uint32_t, m);
+                const uint32_t bits = __float_as_uint(fmaxf(bf16_lo(w), bf16_hi(w)) * b_sum) >> 23;
+                g.e = fmaxf(g.e, bits < 255u ? (float)((int)bits - 126) : -200.f);
+            }
+        } else if constexpr (part == 1) {
+            g.ep = max(-100, min(126, (int)max_over_groups(max_over_row(g.e))));
+        } else if constexpr (part == 2) {
+            if (lane == 0) page_exp[(tile & 1) * 4 + wave] = g.ep;
+            g.ks = __uint_as_float((uint32_t)max(0, min(254, (int)ke - g.ep)) << 23);
+            g.inv = __uint_as_float((uint32_t)(127 - g.ep) << 23);
+            g.vs = f32x4{f8_scale(ve & 255u), f8_scale((ve >> 8) & 255u), f8_scale((ve >> 16) & 255u), f8_scale(ve >> 24)};
+        } else if constexpr (part < 11) {
+            constexpr int i = part - 3;  // word i: dims 32 (i / 2) + 16 (i % 2) + col
+            const uint32_t w = vw[i / 4][i % 4];
+            const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.f, true);
+            st64(g.vd + (i / 2) * 1024 + (i % 2) * 256, u32x2{pack_bf16(lo.x * g.vs.x, lo.y * g.vs.y), pack_bf16(hi.x * g.vs.z, hi.y * g.vs.w)});
+        } else if constexpr (part == 11) {
+            if constexpr (R > 0) {
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    g.ck[t] = u32x2{pack_bf16(bf16_lo(c[t].x) * g.inv, bf16_hi(c[t].x) * g.inv), pack_bf16(bf16_lo(c[t].y) * g.inv, bf16_hi(c[t].y) * g.inv)};
+                    st64(g.cd + (t / 2) * 1024 + (t % 2) * 256, u32x2{c[t].z, c[t].w});
+                }
+            }
+        } else if constexpr (part < 28) {
+            constexpr int i = (part - 12) / 4, s = (part - 12) % 4;  // tiles m and m + 4 (rotate-half partners), m = 2 kk + w
+            constexpr int m = i, kk = i / 2, w = i % 2;
+            if constexpr (s == 0) {
+                if constexpr (R > 0) {
+                    g.x = low_rank(g, m, ROPE ? f32x4{0, 0, 0, 0} : base_key(g, m));
+                    g.y = low_rank(g, m + 4, ROPE ? f32x4{0, 0, 0, 0} : base_key(g, m + 4));
+                } else {
+                    g.x = base_key(g, m);
+                    g.y = base_key(g, m + 4);
+                }
+            } else if constexpr (s == 1) {
+                if constexpr (ROPE) {
+                    g.bx = base_key(g, m);
+                    g.by = base_key(g, m + 4);
+                }
+            } else if constexpr (s == 2) {
+                f32x4 x = g.x, y = g.y;
+                if constexpr (ROPE) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        x[j] = __builtin_fmaf(g.x[j], cs[m][j], __builtin_fmaf(-g.y[j], sn[m][j], g.bx[j]));
+                        y[j] = __builtin_fmaf(g.y[j], cs[m][j], __builtin_fmaf(g.x[j], sn[m][j], g.by[j]));
+                    }
+                }
+                g.pk[0][w] = u32x2{pack_f16(x.x, x.y), pack_f16(x.z, x.w)};
+                g.pk[1][w] = u32x2{pack_f16(y.x, y.y), pack_f16(y.z, y.w)};
+            } else if constexpr (w == 1) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) st128(g.kd + (kk + 2 * j) * 2048, u32x4{g.pk[j][0].x, g.pk[j][0].y, g.pk[j][1].x, g.pk[j][1].y});
+            }
+        } else if constexpr (part == 28) {
+            request(tile + 1);
+        }
+    };
+
+    // ---- queries (B operand: lane = row, dims 32 kk + 4 g + 0..3 and 16 further, g = 2 (st % 2) + hh), fp16 times 2^-eq ----
+    int row_tok[2], eq[2];
+    u32x4 qf[2][8];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+        const int rr = wave * 64 + rb * 32 + r32, tk = tok_begin + rr / G;
+        const bool ok = tk < nq;
+        row_tok[rb] = ok ? tk : -1;
+        const uint16_t *qr = p.q + ((int64_t)(q0 + (ok ? tk : 0)) * p.hq + h * G + rr % G) * D;
+        float big = 0.f;
+#pragma unroll
+        for (int st = 0; st < 8; ++st) {
+            const int dm = 32 * (st / 2) + 4 * (2 * (st % 2) + hh);
+            u32x4 v = {0, 0, 0, 0};
+            if (ok) {
+                const u32x2 lo = ldg64(qr + dm), hi = ldg64(qr + dm + 16);
+                v = u32x4{lo.x, lo.y, hi.x, hi.y};
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) big = fmaxf(big, fmaxf(fabsf(bf16_lo(v[i])), fabsf(bf16_hi(v[i]))));
+            qf[rb][st] = v;
+        }
+        eq[rb] = max(-100, min(126, (int)(__float_as_uint(max_over_halves(big)) >> 23) - 126));
+        const float inv = __uint_as_float((uint32_t)(127 - eq[rb]) << 23);
+#pragma unroll
+        for (int st = 0; st < 8; ++st)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) qf[rb][st][i] = pack_f16(bf16_lo(qf[rb][st][i]) * inv, bf16_hi(qf[rb][st][i]) * inv);
+        if (rb == 0 || NRB < 2) {  // from here on in accumulation registers
+#pragma unroll
+            for (int st = 0; st < 8; ++st) asm("" : "+a"(qf[rb][st]));
+        }
+    }
+    request(0);
+    if constexpr (R > 0) {
+        // B_K^T fragments: lane (c, g) of (tile t, column tile m) holds B_K[16t + 4g + 0..3][16m + c]; sums of the ranks' largest
+        const uint16_t *bk = p.lora_b + (int64_t)ad * 2 * R * n + (int64_t)h * D;
+        float mine = 0.f;
+        for (int rho = wave; rho < R; rho += WAVES) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(bk + (int64_t)rho * n + 2 * lane);
+            mine += max_over_groups(max_over_row(fmaxf(fabsf(bf16_lo(w)), fabsf(bf16_hi(w)))));
+        }
+        float *part = reinterpret_cast<float *>(lds + S::E_OFF);
+        if (lane == 0) part[wave] = mine * 1.4143f;
+        for (int idx = threadIdx.x; idx < RT * 512; idx += 64 * WAVES) {
+            const int ln = idx & 63, m = (idx >> 6) & 7, t = idx >> 9;
+            uint32_t w[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int r0 = 16 * t + 4 * (ln >> 4) + 2 * j;
+                const uint16_t lo = r0 < R ? bk[(int64_t)r0 * n + 16 * m + (ln & 15)] : (uint16_t)0;
+                const uint16_t hi = r0 + 1 < R ? bk[(int64_t)(r0 + 1) * n + 16 * m + (ln & 15)] : (uint16_t)0;
+                w[j] = (uint32_t)lo | ((uint32_t)hi << 16);
+            }
+            st64(lds0 + S::B_OFF + idx * 8, u32x2{w[0], w[1]});
+        }
+        if constexpr (LROW) {  // rows 16..31 of the rank block: ones, for the launch
+            for (int idx = threadIdx.x; idx < 3 * 4 * 64; idx += 64 * WAVES)
+                if (idx & 16) st128(lds0 + S::C_OFF + idx * 16, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) b_sum += part[w];
+        __syncthreads();
+    }
+
+    f32x16 oacc[4][2], racc[NRBX][2];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) oacc[b][0] = oacc[b][1] = f32x16{};
+#pragma unroll
+    for (int b = 0; b < NRBX; ++b) racc[b][0] = racc[b][1] = f32x16{};
+    f32x16 s[2];  // scores of 32 keys
+    float m_run[2] = {kNegInf, kNegInf}, lsum[2] = {0.f, 0.f};
+    const float cl = p.scale_log2;
+
+    // One step: PV: values of block pv_kb of tile pv_tile with the weights pf_in, beside (EXP) the weights of the scores s (32 keys from
+    // key0; page exponents at pe) into pf_out; then QK: scores of block qk_kb of tile qk_tile into s, beside (STAGE) the first or second
+    // half of the staging of tile st_tile.
+    constexpr int NP = 8 + 2 * NRB;
+    auto step = [&](auto exp_tag, auto qk_tag, auto pv_tag, auto stage_tag, u32x4 (&pf_in)[2][2], u32x4 (&pf_out)[2][2], int key0, int pe, int qk_tile,
+                    int qk_kb, int pv_tile, int pv_kb, Staging &g, int st_tile) __attribute__((always_inline)) {
+        constexpr bool EXP = decltype(exp_tag)::value, QK = decltype(qk_tag)::value, PV = decltype(pv_tag)::value;
+        constexpr int STAGE = decltype(stage_tag)::value;  // 0: none, 1: first half of the parts, 2: second half
+        const uint32_t ka = lds0 + (qk_tile & 1) * 16384 + qk_kb * 8192 + lane * 16;
+        const uint32_t va = lds0 + S::V_OFF + (pv_tile % 3) * 16384 + pv_kb * 8192 + lane * 16;
+        const uint32_t ca = lds0 + S::C_OFF + (pv_tile % 3) * S::C_TILE + pv_kb * 2 * NRB * 1024 + lane * 16;
+        // product slots: those of the values (page i / (4 + NRB), block i % (4 + NRB)), then those of the scores
+        auto frag = [&](auto slot_tag) __attribute__((always_inline)) -> u32x4 {
+            constexpr int slot = decltype(slot_tag)::value;
+            if constexpr (slot >= NP) {
+                return QK ? lds_load(ka + (slot - NP) * 1024) : u32x4{};
+            } else {
+                constexpr int pg = slot / (4 + NRB), b = slot % (4 + NRB);
+                if constexpr (!PV) return u32x4{};
+                return b < 4 ? lds_load(va + pg * 4096 + b * 1024) : lds_load(ca + (pg * NRB + b - 4) * 1024);
+            }
+        };
+        auto product = [&](auto slot_tag, const u32x4 &f) __attribute__((always_inline)) {
+            constexpr int slot = decltype(slot_tag)::value;
+            if constexpr (slot >= NP) {
+                if constexpr (QK) {
+                    constexpr int i = slot - NP;
+                    score_product<i == 0, true>(s[0], f, qf[0][i]);
+                    score_product<i == 0, (NRB < 2)>(s[1], f, qf[1][i]);
+                }
+            } else if constexpr (PV) {
+                constexpr int pg = slot / (4 + NRB), b = slot % (4 + NRB);
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb) {
+                    if constexpr (b < 4) oacc[b][rb] = mfma32x32(f, pf_in[pg][rb], oacc[b][rb]);
+                    else racc[b - 4][rb] = mfma32x32(f, pf_in[pg][rb], racc[b - 4][rb]);
+                }
+            }
+        };
+        float f[2][2], mx[2], alpha[2], tsum[2] = {0.f, 0.f};  // f [page][row block]
+        bool moved = false;
+        if constexpr (EXP) {
+            score_wait(s);
+            const int e0 = page_exp[pe], e1 = page_exp[pe + 1];
+            if (key0 + 31 > P0 + tok_begin) {  // causal mask
+#pragma unroll
+                for (int rb = 0; rb < 2; ++rb) {
+                    const int lim = row_tok[rb] < 0 ? -1 : P0 + row_tok[rb] - key0 - 4 * hh;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[rb][i] = 8 * (i / 4) + i % 4 <= lim ? s[rb][i] : kNegInf;
+                }
+            }
+#pragma unroll
+            for (int rb = 0; rb < 2; ++rb) {  // neither 0 nor infinite: masked scores and zeros stay
+                f[0][rb] = fminf(fmaxf(ldexpf(cl, e0 + eq[rb]), 1.2e-38f), 3e38f);
+                f[1][rb] = fminf(fmaxf(ldexpf(cl, e1 + eq[rb]), 1.2e-38f), 3e38f);
+            }
+        }
+        auto maxima = [&](int rb) __attribute__((always_inline)) {
+            float x0 = fmaxf(s[rb][0], s[rb][1]), x1 = fmaxf(s[rb][8], s[rb][9]);
+#pragma unroll
+            for (int i = 2; i < 8; ++i) {
+                x0 = fmaxf(x0, s[rb][i]);
+                x1 = fmaxf(x1, s[rb][8 + i]);
+            }
+            mx[rb] = max_over_halves(fmaxf(x0 * f[0][rb], x1 * f[1][rb]));
+        };
+        auto weights = [&](auto pair_tag) __attribute__((always_inline)) {  // pair w of 16: row block w / 8, values 2 (w % 8), + 1
+            constexpr int w = decltype(pair_tag)::value, rb = w / 8, i = 2 * (w % 8), pg = i / 8;
+            const float m_use = m_run[rb] == kNegInf ? 0.f : m_run[rb];
+            const float e0 = fast_exp2(__builtin_fmaf(s[rb][i], f[pg][rb], -m_use)), e1 = fast_exp2(__builtin_fmaf(s[rb][i + 1], f[pg][rb], -m_use));
+            const uint32_t pk = pack_bf16(e0, e1);
+            pf_out[pg][rb][(i % 8) / 2] = pk;
+            if constexpr (!LROW) tsum[rb] = add_bf16_pair(pk, tsum[rb]);  // the weights as the products take them: their rounding cancels in O / l
+        };
+        constexpr int PRE = 4, SLOTS = NP + 8, FIRST = 3;  // operands read ahead; first slot with weights beside it
+        u32x4 fr[PRE];
+        each<PRE>([&](auto q) __attribute__((always_inline)) { fr[q.value] = frag(q); });
+        fence();
+        each<SLOTS>([&](auto slot_tag) __attribute__((always_inline)) {
+            constexpr int slot = decltype(slot_tag)::value;
+            product(slot_tag, fr[slot % PRE]);
+            if constexpr (slot + PRE < SLOTS) fr[slot % PRE] = frag(std::integral_constant<int, slot + PRE>{});
+            if constexpr (EXP && slot < NP) {
+                if constexpr (slot == 0) maxima(0);
+                if constexpr (slot == 1) maxima(1);
+                if constexpr (slot == 2) {
+                    const float up = fmaxf(mx[0] - m_run[0], mx[1] - m_run[1]);  // (NaN for a row that has seen no key: -inf - -inf)
+                    moved = __builtin_amdgcn_ballot_w64(up > kLazyRescale) != 0;
+                    if (moved) {
+#pragma unroll
+                        for (int rb = 0; rb < 2; ++rb) {
+                            const float m_new = fmaxf(m_run[rb], mx[rb]);
+                            alpha[rb] = fast_exp2(m_run[rb] - (m_new == kNegInf ? 0.f : m_new));
+                            m_run[rb] = m_new;
+                        }
+                    }
+                }
+                if constexpr (slot >= FIRST) {
+                    constexpr int w0 = 16 * (slot - FIRST) / (NP - FIRST), w1 = 16 * (slot + 1 - FIRST) / (NP - FIRST);
+                    each<w1 - w0>([&](auto q) __attribute__((always_inline)) { weights(std::integral_constant<int, w0 + q.value>{}); });
+                }
+            }
+            if constexpr (EXP && slot == NP - 1) {
+                if (moved) {
+#pragma unroll
+                    for (int rb = 0; rb < 2; ++rb) {
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {  // (one block at a time: they come to vector registers for it)
+                            oacc[b][rb] *= alpha[rb];
+                            fence();
+                        }
+#pragma unroll
+                        for (int b = 0; b < NRB; ++b) {
+                            racc[b][rb] *= alpha[rb];
+                            fence();
+                        }
+                        lsum[rb] *= alpha[rb];
+                    }
+                }
+                if constexpr (!LROW) {
+                    lsum[0] += tsum[0];
+                    lsum[1] += tsum[1];
+                }
+            }
+            if constexpr (STAGE > 0 && slot >= NP) {
+                constexpr int HALF = PARTS / 2, q = slot - NP, p0 = HALF * q / 8, p1 = HALF * (q + 1) / 8;
+                each<p1 - p0>([&](auto i) __attribute__((always_inline)) {
+                    stage_part(g, st_tile, std::integral_constant<int, (STAGE - 1) * HALF + p0 + i.value>{});
+                });
+            }
+            fence();
+        });
+    };
+    using T = std::true_type;
+    using F = std::false_type;
+    using N0 = std::integral_constant<int, 0>;
+    using N1 = std::integral_constant<int, 1>;
+    using N2 = std::integral_constant<int, 2>;
+    Staging g;
+    u32x4 pa[2][2], pb[2][2];  // weights of a tile's second and first half [page][row block]
+
+    each<PARTS>([&](auto i) __attribute__((always_inline)) { stage_part(g, 0, i); });  // (requests tile 1)
+    __syncthreads();
+    // tile 0: no values yet
+    step(F{}, T{}, F{}, N1{}, pa, pb, 0, 0, 0, 0, 0, 0, g, 1);
+    step(T{}, T{}, F{}, N2{}, pa, pb, 0, 0, 0, 1, 0, 0, g, 1);
+    for (int u = 1; u < n_tiles; ++u) {
+        __syncthreads();  // tile u is staged, tile u - 1's keys and tile u - 2's values are read
+        step(T{}, T{}, T{}, N1{}, pb, pa, (u - 1) * TILE_KEYS + 32, ((u - 1) & 1) * 4 + 2, u, 0, u - 1, 0, g, u + 1);
+        step(T{}, T{}, T{}, N2{}, pa, pb, u * TILE_KEYS, (u & 1) * 4, u, 1, u - 1, 1, g, u + 1);
+    }
+    // the last tile's second half, and its values
+    step(T{}, F{}, T{}, N0{}, pb, pa, (n_tiles - 1) * TILE_KEYS + 32, ((n_tiles - 1) & 1) * 4 + 2, 0, 0, n_tiles - 1, 0, g, 0);
+    step(F{}, F{}, T{}, N0{}, pa, pb, 0, 0, 0, 0, n_tiles - 1, 1, g, 0);
+    __syncthreads();
+
+    // ---- epilogue: O = (acc + acc_r . B_V[h]) / l; lane: row r32, dims 32 b + 8 (i / 4) + 4 hh + i % 4 ----
+    float l_run[2];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) l_run[rb] = LROW ? racc[0][rb][8] : lsum[rb] + __shfl_xor(lsum[rb], 32);
+    if constexpr (R > 0) {
+        float *bv = reinterpret_cast<float *>(lds), *acc = bv + R * D;
+        const uint16_t *src = p.lora_b + ((int64_t)ad * 2 + 1) * R * n + (int64_t)h * D;
+        for (int e = threadIdx.x; e < R * D / 2; e += 64 * WAVES) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(src + (int64_t)(e / (D / 2)) * n + 2 * (e % (D / 2)));
+            bv[2 * e] = bf16_lo(w);
+            bv[2 * e + 1] = bf16_hi(w);
+        }
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+            for (int b = 0; b < NRB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int rho = 32 * b + 8 * (i / 4) + 4 * hh + i % 4;
+                    if (rho < R) acc[(wave * 64 + rb * 32 + r32) * (R + 1) + rho] = racc[b][rb][i];
+                }
+        __syncthreads();
+#pragma unroll 2
+        for (int rho = 0; rho < R; ++rho) {
+            const float x0 = acc[(wave * 64 + r32) * (R + 1) + rho], x1 = acc[(wave * 64 + 32 + r32) * (R + 1) + rho];
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(bv + rho * D + 32 * b + 8 * i + 4 * hh);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        oacc[b][0][4 * i + j] += x0 * v[j];
+                        oacc[b][1][4 * i + j] += x1 * v[j];
+                    }
+                }
+        }
+    }
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+        if (row_tok[rb] < 0) continue;
+        const float inv = l_run[rb] > 0.f ? 1.f / l_run[rb] : 0.f;
+        uint16_t *o = p.out + ((int64_t)(q0 + row_tok[rb]) * p.hq + h * G + (wave * 64 + rb * 32 + r32) % G) * D;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 v = {oacc[b][rb][4 * i] * inv, oacc[b][rb][4 * i + 1] * inv, oacc[b][rb][4 * i + 2] * inv, oacc[b][rb][4 * i + 3] * inv};
+                *reinterpret_cast<u32x2 *>(o + 32 * b + 8 * i + 4 * hh) = pack4(v);
+            }
+    }
+}
+
+template <int R, int G, bool ROPE>
+__global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_stream_kernel(PrefillArgs p) {
+    constexpr int TPW = ROWS / G;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[Lay<R>::BYTES > Lay<0>::BYTES ? Lay<R>::BYTES : Lay<0>::BYTES];
+    const int bpa = p.blocks_per_agent_head;
+    const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
+    const int pair = (local / bpa) * kXcds + xcd, qb = local % bpa;
+    if (pair >= p.n_agents * p.hkv) return;
+    const int a = pair / p.hkv, h = pair % p.hkv;
+    const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
+    const int tok_begin = qb * TPW;
+    if (qb == bpa - 1 && nq > bpa * TPW) poison_unreached_rows(p, q0, nq, h, G, bpa * TPW);
+    if (tok_begin >= nq) return;
+    if (R > 0 && p.adapter_idx[a] >= 0) block<R, G, ROPE>(p, lds, a, h, tok_begin);
+    else block<0, G, false>(p, lds, a, h, tok_begin);
+}
+
+template <int R, int G, bool ROPE>
+hipError_t launch(const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+    const int pairs = (pa.n_agents * pa.hkv + kXcds - 1) / kXcds * kXcds;
+    // timing events carry the kernel's own start and end timestamps (set by the launch)
+    hipEvent_t e0 = ev ? static_cast<hipEvent_t>(ev[0]) : nullptr, e1 = ev ? static_cast<hipEvent_t>(ev[1]) : nullptr;
+    hipExtLaunchKernelGGL((prefill_fp8_stream_kernel<R, G, ROPE>), dim3(pairs * pa.blocks_per_agent_head), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
+    return hipGetLastError();
+}
+
+template <int G>
+hipError_t dispatch(int r, bool rope, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+    switch (r) {
+    case 0: return launch<0, G, false>(pa, st, ev);
+    case 8: return rope ? launch<8, G, true>(pa, st, ev) : launch<8, G, false>(pa, st, ev);
+    case 16: return rope ? launch<16, G, true>(pa, st, ev) : launch<16, G, false>(pa, st, ev);
+    case 32: return rope ? launch<32, G, true>(pa, st, ev) : launch<32, G, false>(pa, st, ev);
+    case 64: return rope ? launch<64, G, true>(pa, st, ev) : launch<64, G, false>(pa, st, ev);
+    default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_fp8_stream(int r, int g, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+    const bool rope = r > 0 && pa.rope_cos;
+    return g == 4 ? dispatch<4>(r, rope, pa, st, ev) : dispatch<8>(r, rope, pa, st, ev);
+}
+
+}  // namespace fkvp
