@@ -64,6 +64,13 @@ __device__ __forceinline__ void score_product(f32x16 &s, const u32x4 &a, const u
 }
 __device__ __forceinline__ void score_wait(f32x16 (&s)[2]) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1])); }
 
+// (as an instruction: the compiler would first make a quiet NaN of every value that comes out of one of its own making)
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+
 // f(integral_constant 0), f(1), ..., f(N - 1): steps whose index selects code, without leaving the unrolling to the optimiser's limits.
 template <int... I, class F>
 __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F &&f) {
@@ -361,21 +368,15 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
                 return b < 4 ? lds_load(va + pg * 4096 + b * 1024) : lds_load(ca + (pg * NRB + b - 4) * 1024);
             }
         };
-        auto product = [&](auto slot_tag, const u32x4 &f) __attribute__((always_inline)) {
-            constexpr int slot = decltype(slot_tag)::value;
+        auto product = [&](auto slot_tag, auto rb_tag, const u32x4 &f) __attribute__((always_inline)) {
+            constexpr int slot = decltype(slot_tag)::value, rb = decltype(rb_tag)::value;
             if constexpr (slot >= NP) {
-                if constexpr (QK) {
-                    constexpr int i = slot - NP;
-                    score_product<i == 0, true>(s[0], f, qf[0][i]);
-                    score_product<i == 0, (NRB < 2)>(s[1], f, qf[1][i]);
-                }
+                constexpr int i = slot - NP;
+                if constexpr (QK) score_product<i == 0, (rb == 0 || NRB < 2)>(s[rb], f, qf[rb][i]);
             } else if constexpr (PV) {
                 constexpr int pg = slot / (4 + NRB), b = slot % (4 + NRB);
-#pragma unroll
-                for (int rb = 0; rb < 2; ++rb) {
-                    if constexpr (b < 4) oacc[b][rb] = mfma32x32(f, pf_in[pg][rb], oacc[b][rb]);
-                    else racc[b - 4][rb] = mfma32x32(f, pf_in[pg][rb], racc[b - 4][rb]);
-                }
+                if constexpr (b < 4) oacc[b][rb] = mfma32x32(f, pf_in[pg][rb], oacc[b][rb]);
+                else racc[b - 4][rb] = mfma32x32(f, pf_in[pg][rb], racc[b - 4][rb]);
             }
         };
         float f[2][2], mx[2], alpha[2], tsum[2] = {0.f, 0.f};  // f [page][row block]
@@ -398,34 +399,31 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             }
         }
         auto maxima = [&](int rb) __attribute__((always_inline)) {
-            float x0 = fmaxf(s[rb][0], s[rb][1]), x1 = fmaxf(s[rb][8], s[rb][9]);
-#pragma unroll
-            for (int i = 2; i < 8; ++i) {
-                x0 = fmaxf(x0, s[rb][i]);
-                x1 = fmaxf(x1, s[rb][8 + i]);
-            }
+            float x0 = max3(s[rb][0], s[rb][1], s[rb][2]), x1 = max3(s[rb][8], s[rb][9], s[rb][10]);
+            x0 = max3(x0, s[rb][3], s[rb][4]);
+            x1 = max3(x1, s[rb][11], s[rb][12]);
+            x0 = max3(x0, max3(s[rb][5], s[rb][6], s[rb][7]), x0);
+            x1 = max3(x1, max3(s[rb][13], s[rb][14], s[rb][15]), x1);
             mx[rb] = max_over_halves(fmaxf(x0 * f[0][rb], x1 * f[1][rb]));
         };
         auto weights = [&](auto pair_tag) __attribute__((always_inline)) {  // pair w of 16: row block w / 8, values 2 (w % 8), + 1
             constexpr int w = decltype(pair_tag)::value, rb = w / 8, i = 2 * (w % 8), pg = i / 8;
             const float m_use = m_run[rb] == kNegInf ? 0.f : m_run[rb];
             const float e0 = fast_exp2(__builtin_fmaf(s[rb][i], f[pg][rb], -m_use)), e1 = fast_exp2(__builtin_fmaf(s[rb][i + 1], f[pg][rb], -m_use));
-            const uint32_t pk = pack_bf16(e0, e1);
+            uint32_t pk = pack_bf16(e0, e1);
+            asm volatile("" : "+v"(pk));  // stays here: otherwise the compiler moves the weights past the branch below, behind the products
             pf_out[pg][rb][(i % 8) / 2] = pk;
             if constexpr (!LROW) tsum[rb] = add_bf16_pair(pk, tsum[rb]);  // the weights as the products take them: their rounding cancels in O / l
         };
-        constexpr int PRE = 4, SLOTS = NP + 8, FIRST = 3;  // operands read ahead; first slot with weights beside it
-        u32x4 fr[PRE];
-        each<PRE>([&](auto q) __attribute__((always_inline)) { fr[q.value] = frag(q); });
-        fence();
-        each<SLOTS>([&](auto slot_tag) __attribute__((always_inline)) {
-            constexpr int slot = decltype(slot_tag)::value;
-            product(slot_tag, fr[slot % PRE]);
-            if constexpr (slot + PRE < SLOTS) fr[slot % PRE] = frag(std::integral_constant<int, slot + PRE>{});
-            if constexpr (EXP && slot < NP) {
-                if constexpr (slot == 0) maxima(0);
-                if constexpr (slot == 1) maxima(1);
-                if constexpr (slot == 2) {
+        // beside product i (two per operand, so that vector work fills the time of each: a wave that issues two products in a row
+        // stands still for the length of the first)
+        constexpr int PRE = 4, SLOTS = NP + 8, FIRST = 4;  // operands read ahead; first product with weights beside it
+        auto beside = [&](auto product_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(product_tag)::value;
+            if constexpr (EXP && i < 2 * NP) {
+                if constexpr (i == 1) maxima(0);
+                if constexpr (i == 2) maxima(1);
+                if constexpr (i == 3) {
                     const float up = fmaxf(mx[0] - m_run[0], mx[1] - m_run[1]);  // (NaN for a row that has seen no key: -inf - -inf)
                     moved = __builtin_amdgcn_ballot_w64(up > kLazyRescale) != 0;
                     if (moved) {
@@ -437,40 +435,51 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
                         }
                     }
                 }
-                if constexpr (slot >= FIRST) {
-                    constexpr int w0 = 16 * (slot - FIRST) / (NP - FIRST), w1 = 16 * (slot + 1 - FIRST) / (NP - FIRST);
+                if constexpr (i >= FIRST) {
+                    constexpr int n = 2 * NP - FIRST, w0 = 16 * (i - FIRST) / n, w1 = 16 * (i + 1 - FIRST) / n;
                     each<w1 - w0>([&](auto q) __attribute__((always_inline)) { weights(std::integral_constant<int, w0 + q.value>{}); });
                 }
-            }
-            if constexpr (EXP && slot == NP - 1) {
-                if (moved) {
+                if constexpr (i == 2 * NP - 1) {
+                    if (moved) {
 #pragma unroll
-                    for (int rb = 0; rb < 2; ++rb) {
+                        for (int rb = 0; rb < 2; ++rb) {
 #pragma unroll
-                        for (int b = 0; b < 4; ++b) {  // (one block at a time: they come to vector registers for it)
-                            oacc[b][rb] *= alpha[rb];
-                            fence();
+                            for (int b = 0; b < 4; ++b) {  // (one block at a time: they come to vector registers for it)
+                                oacc[b][rb] *= alpha[rb];
+                                fence();
+                            }
+#pragma unroll
+                            for (int b = 0; b < NRB; ++b) {
+                                racc[b][rb] *= alpha[rb];
+                                fence();
+                            }
+                            lsum[rb] *= alpha[rb];
                         }
-#pragma unroll
-                        for (int b = 0; b < NRB; ++b) {
-                            racc[b][rb] *= alpha[rb];
-                            fence();
-                        }
-                        lsum[rb] *= alpha[rb];
+                    }
+                    if constexpr (!LROW) {
+                        lsum[0] += tsum[0];
+                        lsum[1] += tsum[1];
                     }
                 }
-                if constexpr (!LROW) {
-                    lsum[0] += tsum[0];
-                    lsum[1] += tsum[1];
-                }
             }
-            if constexpr (STAGE > 0 && slot >= NP) {
-                constexpr int HALF = PARTS / 2, q = slot - NP, p0 = HALF * q / 8, p1 = HALF * (q + 1) / 8;
-                each<p1 - p0>([&](auto i) __attribute__((always_inline)) {
-                    stage_part(g, st_tile, std::integral_constant<int, (STAGE - 1) * HALF + p0 + i.value>{});
+            if constexpr (STAGE > 0 && i >= 2 * NP) {
+                constexpr int HALF = PARTS / 2, q = i - 2 * NP, p0 = HALF * q / 16, p1 = HALF * (q + 1) / 16;
+                each<p1 - p0>([&](auto k) __attribute__((always_inline)) {
+                    stage_part(g, st_tile, std::integral_constant<int, (STAGE - 1) * HALF + p0 + k.value>{});
                 });
             }
             fence();
+        };
+        u32x4 fr[PRE];
+        each<PRE>([&](auto q) __attribute__((always_inline)) { fr[q.value] = frag(q); });
+        fence();
+        each<SLOTS>([&](auto slot_tag) __attribute__((always_inline)) {
+            constexpr int slot = decltype(slot_tag)::value;
+            product(slot_tag, std::integral_constant<int, 0>{}, fr[slot % PRE]);
+            beside(std::integral_constant<int, 2 * slot>{});
+            product(slot_tag, std::integral_constant<int, 1>{}, fr[slot % PRE]);
+            if constexpr (slot + PRE < SLOTS) fr[slot % PRE] = frag(std::integral_constant<int, slot + PRE>{});
+            beside(std::integral_constant<int, 2 * slot + 1>{});
         });
     };
     using T = std::true_type;
