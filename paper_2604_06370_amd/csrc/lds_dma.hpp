@@ -45,6 +45,9 @@ __device__ __forceinline__ u32x4 buf_load16(i32x4 rsrc, int voff) {
 __device__ __forceinline__ u32x4 buf_load16_at(i32x4 rsrc, int voff, int soff) {
     return __builtin_bit_cast(u32x4, raw_buffer_load_b128(rsrc, voff, soff, kCacheDefault));
 }
+// Eight bytes, at a further uniform offset.
+__device__ u32x2 raw_buffer_load_b64(i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.v2i32");
+__device__ __forceinline__ u32x2 buf_load8_at(i32x4 rsrc, int voff, int soff) { return raw_buffer_load_b64(rsrc, voff, soff, kCacheDefault); }
 // Copy: lane i's 16 bytes at byte offset voff of the resource land at dst + 16 i.  The
 // instruction's immediate offset stays 0 (it would shift the LDS destination as well).
 template <int POLICY = kCacheDefault>

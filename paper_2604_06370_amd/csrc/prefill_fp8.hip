@@ -7,8 +7,8 @@
 //               matrix-core operands in LDS, where all waves read them: a value is converted once per workgroup.
 //               K = K_base + RoPE_p(B_K^T C_K^T) (without tables no rotation), V = code * 2^E.
 //   every wave  S^T = K Q^T, causal mask + online softmax, O^T += V^T P^T, acc_r^T += C_V^T P^T over its 8 NRG / 8 pages
-// and at the end the key groups' rows are merged and O = (O + acc_r . B_V[h]) / l (Eq. 4) is written in bf16.  The launch takes
-// fewer rows per workgroup where 256 leave compute units idle: the rest of a workgroup's waves then share its keys.
+// and at the end the key groups' rows are merged and O = (O + acc_r . B_V[h]) / l (Eq. 4) is written in bf16.  This is the kernel of
+// workgroups of 128, 64 and 32 rows, where 256 would leave compute units idle; prefill_fp8_stream.hip has the one of 256.
 //
 // K and Q are fp16 here, 11 significant bits: the sum of a base key, exact in four bits, and its low-rank part would
 // lose what bf16 keeps of it alone (error of the result 5.6e-3 with bf16 keys at 8B heads, rank 16, over 9000 tokens, 2-norm; 2.2e-3 in
@@ -88,9 +88,23 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     uint32_t ke, ve;
     u32x4 c[RTX];
     f32x4 cs[4], sn[4];
-    auto request = [&](int round) __attribute__((always_inline)) {
-        const int pg = min(ROUND_PAGES * round + wave, n_pages - 1);  // pages past the sequence repeat its last one; their keys are masked
-        const unsigned char *page = base + (int64_t)btb[pg] * f8_page_bytes(hkv);
+    // Page ids of this wave's pages of 64 rounds, one per lane, and of the 64 after them: an id read where it is used would hold up the wave.
+    auto ids = [&](int chunk, int &b, int &r) __attribute__((always_inline)) {
+        const int pg = min((64 * chunk + lane) * ROUND_PAGES + wave, n_pages - 1);  // pages past the sequence repeat its last one; their keys are masked
+        b = btb[pg];
+        r = R > 0 ? btr[pg] : 0;
+    };
+    int idb, idr, idb_next, idr_next;
+    ids(0, idb, idr);
+    ids(1, idb_next, idr_next);
+    auto request = [&](int round) __attribute__((always_inline)) {  // rounds in order, from 0
+        if (__builtin_expect(round > 0 && (round & 63) == 0, 0)) {
+            idb = idb_next;
+            idr = idr_next;
+            ids((round >> 6) + 1, idb_next, idr_next);
+        }
+        const int pg = min(ROUND_PAGES * round + wave, n_pages - 1);
+        const unsigned char *page = base + (int64_t)__builtin_amdgcn_readlane(idb, round & 63) * f8_page_bytes(hkv);
         const unsigned char *blk = page + (int64_t)h * kF8HeadBytes + lane * 16;
         const unsigned char *ex = page + f8_exp_off(hkv, h);
 #pragma unroll
@@ -102,7 +116,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
         ve = *reinterpret_cast<const uint32_t *>(ex + PS + 4 * grp);
         if constexpr (R > 0) {
             if (use_res) {
-                const uint16_t *rb = p.res_kv + (int64_t)btr[pg] * (RT * 512) + lane * 8;
+                const uint16_t *rb = p.res_kv + (int64_t)__builtin_amdgcn_readlane(idr, round & 63) * (RT * 512) + lane * 8;
 #pragma unroll
                 for (int t = 0; t < RT; ++t) c[t] = ldg128(rb + t * 512);
             }
@@ -388,10 +402,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
 
     request(0);
     for (int round = 0; round < n_rounds; ++round) {
-        __syncthreads();  // the last round is read, the B_K^T fragments and rank sums are written (and read)
+        lds_fence_barrier();  // the last round is read, the B_K^T fragments and rank sums are written (and read)
         stage(round);
         if (round + 1 < n_rounds) request(round + 1);
-        __syncthreads();
+        lds_fence_barrier();  // (not one that waits for the loads in flight)
 #pragma unroll
         for (int s = 0; s < GP; s += CP) {
             const int key0 = round * ROUND_KEYS + (kg * GP + s) * PS;
@@ -474,7 +488,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
 }
 
 // Rows per workgroup: the most (of 256, 128, 64, 32) whose workgroups still fill every compute unit of the fullest XCD (an (agent,
-// KV head) pair keeps to one XCD), else 32.
+// KV head) pair keeps to one XCD), else 32.  Four chunks of up to 250 tokens over 35k, 8B heads: 128 rows 1019 us, 256 rows 1214 us;
+// eight of up to 1024 over 9.5k, RoPE: 256 rows 1698 us, 128 rows 2168 us.
 int rows_of(int64_t pairs, int64_t max_q, int g) {
     const int64_t per_xcd = (pairs + kXcds - 1) / kXcds;
     for (int rows = 256; rows > 32; rows /= 2)
@@ -494,7 +509,6 @@ hipError_t launch(const PrefillArgs &pa, hipStream_t st, void *const *ev) {
 template <int R, int G>
 hipError_t dispatch_rows(int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     switch (rows) {
-    case 256: return launch<R, G, 8>(pa, st, ev);
     case 128: return launch<R, G, 4>(pa, st, ev);
     case 64: return launch<R, G, 2>(pa, st, ev);
     default: return launch<R, G, 1>(pa, st, ev);
@@ -518,7 +532,7 @@ hipError_t dispatch(int r, int rows, const PrefillArgs &pa, hipStream_t st, void
 hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev) {
     const int rows = rows_of((int64_t)pa.n_agents * pa.hkv, max_q, g);
     pa.blocks_per_agent_head = (int)((max_q * g + rows - 1) / rows);
-    if (rows == 256) return launch_fp8_stream(r, g, pa, st, ev);
+    if (rows == 256) return launch_fp8_stream(r, g, pa, st, ev);  // (measured beside that kernel)
     return g == 4 ? dispatch<4>(r, rows, pa, st, ev) : dispatch<8>(r, rows, pa, st, ev);
 }
 

@@ -1,17 +1,24 @@
 // ResidualAttention chunked prefill over 8-bit base pages, the kernel of large grids (Section 6 prefill kernel, Algorithm 1 with
 // a block of query rows; fp8_cache.hpp has the page format, prefill_fp8.hip the scales of K and Q and the kernel of small grids).
 //
-// One workgroup of four waves = (agent a, KV head h, block of 256 query rows), 64 rows per wave: every operand that a wave
-// reads from LDS serves two 32x32x16 products, so that a 64-key tile costs 128 KB of LDS reads instead of the 256 KB of eight waves of
-// 32 rows, which takes LDS as long as its products take the matrix cores.  One wave per SIMD, up to 512 registers.
+// One workgroup of eight waves = (agent a, KV head h, block of 256 query rows), 32 rows per wave and two waves per SIMD (within 256
+// registers each): while one wave's products hold the matrix cores the other issues its vector work.  Four waves of 64 rows read
+// half as much from LDS (every operand serves two products) and were slower, 895 against 920 TFLOP/s without adapters, 733 against 752
+// at rank 16 with RoPE and 300 against 700 at rank 64, where their accumulators spilled: alone on its SIMD, a wave's vector instructions
+// wait for its own products.
 //
-// A wave stages one page per tile (four pages): codes and rCache rows come to registers a tile ahead and leave as operands in
-// LDS, K = K_base + RoPE_p(B_K^T C_K^T) in fp16 times 2^-e, V = code * 2^E in bf16, C_V.  The work goes in steps of 32 keys
-// (half a tile); step i issues, product by product in a written order,
-//   matrix cores   O^T += V^T P^T and acc_r^T += C_V^T P^T of step i - 1, S^T = K Q^T of step i + 1
-//   vector ALU     row maxima and weights of step i, and its share of the staging of the next tile
-// so that a wave has both kinds of work at any time; one barrier per tile.  A change of the running maximum rescales the accumulators at the
+// Wave w stages half of page w % 4 of a tile (four pages): the quarters w / 4 and w / 4 + 2 of the head dim, rotate-half partners.
+// Codes and rCache rows come to registers a tile ahead and leave as operands in LDS, K = K_base + RoPE_p(B_K^T C_K^T) in fp16 times
+// 2^-e, V = code * 2^E in bf16, C_V.  The work goes in steps of 32 keys (half a tile); step i issues, product by product in a
+// written order,
+//   O^T += V^T P^T and acc_r^T += C_V^T P^T of step i - 1, beside the row maxima and weights of step i
+//   S^T = K Q^T of step i + 1, beside half of the staging of the next tile
+// so that every product has vector work next to it; one barrier per tile.  A change of the running maximum rescales the accumulators at the
 // end of its step, when the products of the step before, which carry the old one, are in.
+//
+// Measured at 16 chunks of 1024 tokens over 9.5k tokens of context, 8B heads: 950 TFLOP/s without adapters (a large bf16 product of
+// the library: 1140), 905 with rank 16 (prefill_fp8.hip's kernel at 256 rows: 823), 757 with RoPE (712), and 700 at rank 64 with RoPE
+// over 70B heads (511).
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -29,7 +36,7 @@ using namespace fkvk;
 namespace fkvp {
 namespace {
 
-constexpr int D = 128, PS = 16, TILE_KEYS = 64, WAVES = 4, ROWS = 256;
+constexpr int D = 128, PS = 16, TILE_KEYS = 64, WAVES = 8, ROWS = 256;
 constexpr float kNegInf = -INFINITY, kLazyRescale = 8.f;
 
 template <int R>
@@ -50,27 +57,9 @@ __device__ __forceinline__ void st128(uint32_t a, const u32x4 &v) { *reinterpret
 __device__ __forceinline__ void st64(uint32_t a, const u32x2 &v) { *reinterpret_cast<lds64>((uintptr_t)a) = v; }
 __device__ __forceinline__ u32x2 ld64(uint32_t a) { return *reinterpret_cast<const __attribute__((address_space(3))) u32x2 *>((uintptr_t)a); }
 
-// S = A B (FIRST) or S + A B with the scores in vector registers and, BA, the queries in accumulation registers: written as an instruction
-// because the compiler puts the results of all of a kernel's products into one kind of register, and here the 160 to 192 of the
-// outputs belong into accumulation registers while every score is read by vector instructions (a move each).  What the compiler
-// then does not know: two states have to pass between a vector instruction that writes an operand (a copy that the register allocator
-// made, say) and the product, and twelve between the product and a vector instruction that reads its result (score_wait).
-template <bool FIRST, bool BA>
-__device__ __forceinline__ void score_product(f32x16 &s, const u32x4 &a, const u32x4 &b) {
-    if constexpr (FIRST && BA) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "a"(b));
-    else if constexpr (FIRST) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
-    else if constexpr (BA) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "a"(b));
-    else asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_f16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+__device__ __forceinline__ f32x16 mfma32x32_f16(const u32x4 &a, const u32x4 &b, const f32x16 &c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-__device__ __forceinline__ void score_wait(f32x16 (&s)[2]) { asm volatile("s_nop 15\n\ts_nop 3" : "+v"(s[0]), "+v"(s[1])); }
-
-// (as an instruction: the compiler would first make a quiet NaN of every value that comes out of one of its own making)
-__device__ __forceinline__ float max3(float x, float y, float z) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
-    return r;
-}
-
 // f(integral_constant 0), f(1), ..., f(N - 1): steps whose index selects code, without leaving the unrolling to the optimiser's limits.
 template <int... I, class F>
 __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F &&f) {
@@ -102,36 +91,35 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     const unsigned char *base = reinterpret_cast<const unsigned char *>(p.base_kv);
     int *page_exp = reinterpret_cast<int *>(lds + S::E_OFF);  // [2 tiles][page]
 
-    // ---- staging: page `wave` of a tile (pages past the sequence repeat its last one; their keys are masked) ----
-    u32x4 kw[2], vw[2];
+    // ---- staging: half `half` of page pw of a tile (pages past the sequence repeat its last one; their keys are masked): quarters
+    // half and half + 2 of the head dim, whose dims are rotate-half partners ----
+    const int pw = wave & 3, half = wave >> 2;
+    u32x2 kw[2], vw[2];
     uint32_t ke, ve;
     u32x4 c[RTX];
-    f32x4 cs[4], sn[4];
-    auto page_of = [&](int tile) __attribute__((always_inline)) { return min(4 * tile + wave, n_pages - 1); };
+    f32x4 cs[2], sn[2];
+    auto page_of = [&](int tile) __attribute__((always_inline)) { return min(4 * tile + pw, n_pages - 1); };
     // (buffer loads: a scalar base and one lane offset; lane addresses of 64 bits would be kept in registers for the launch)
-    const int off16 = lane * 16, off_ve = PS + 4 * grp, off_ke = col;
+    const int off16 = lane * 16, off8 = lane * 16 + half * 8, off_ve = PS + 4 * grp, off_ke = col;
     // Page ids of this wave's pages of 64 tiles, one per lane, and of the 64 after them: an id read where it is used would hold up the wave.
     auto ids = [&](int chunk, int &b, int &r) __attribute__((always_inline)) {
-        const int pg = min((64 * chunk + lane) * 4 + wave, n_pages - 1);
+        const int pg = min((64 * chunk + lane) * 4 + pw, n_pages - 1);
         b = btb[pg];
         r = R > 0 ? btr[pg] : 0;
     };
     int idb, idr, idb_next, idr_next;
     ids(0, idb, idr);
     ids(1, idb_next, idr_next);
-    auto request = [&](int tile) __attribute__((always_inline)) {  // tiles in order, from 0
-        if (tile > 0 && (tile & 63) == 0) {
+    // What staging takes first (exponents, rCache, V) and last (K) is requested as soon as the tile before has used its registers.
+    // Tiles in order, from 0.
+    auto request = [&](int tile) __attribute__((always_inline)) {
+        if (__builtin_expect(tile > 0 && (tile & 63) == 0, 0)) {
             idb = idb_next;
             idr = idr_next;
             ids((tile >> 6) + 1, idb_next, idr_next);
         }
         const uint64_t page = reinterpret_cast<uint64_t>(base) + (int64_t)__builtin_amdgcn_readlane(idb, tile & 63) * f8_page_bytes(hkv);
         const i32x4 blk = block_rsrc(page + (int64_t)h * kF8HeadBytes, kF8HeadBytes), ex = block_rsrc(page + f8_exp_off(hkv, h), 2 * PS);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            kw[j] = buf_load16_at(blk, off16, 1024 * j);
-            vw[j] = buf_load16_at(blk, off16, kF8Block + 1024 * j);
-        }
         ke = buf_load_u8(ex, off_ke);
         ve = buf_load4(ex, off_ve);
         if constexpr (R > 0) {
@@ -139,54 +127,62 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
 #pragma unroll
             for (int t = 0; t < RT; ++t) c[t] = buf_load16_at(rb, off16, t * 1024);
         }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) vw[j] = buf_load8_at(blk, off8, kF8Block + 1024 * j);
     };
-    auto request_angles = [&](int tile, int m) __attribute__((always_inline)) {  // of frequency tile m
+    auto request_keys = [&](int tile) __attribute__((always_inline)) {  // (after request of the same tile)
+        const uint64_t page = reinterpret_cast<uint64_t>(base) + (int64_t)__builtin_amdgcn_readlane(idb, tile & 63) * f8_page_bytes(hkv);
+        const i32x4 blk = block_rsrc(page + (int64_t)h * kF8HeadBytes, kF8HeadBytes);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) kw[j] = buf_load8_at(blk, off8, 1024 * j);
+    };
+    auto request_angles = [&](int tile, int w) __attribute__((always_inline)) {  // of frequency tile 2 half + w
         if constexpr (ROPE) {
             const int64_t at = (int64_t)page_of(tile) * (PS * D / 2 * 4);
             const i32x4 rc = block_rsrc(reinterpret_cast<uint64_t>(p.rope_cos) + at, PS * D / 2 * 4);
             const i32x4 rs = block_rsrc(reinterpret_cast<uint64_t>(p.rope_sin) + at, PS * D / 2 * 4);
-            cs[m] = __builtin_bit_cast(f32x4, buf_load16_at(rc, off16, 1024 * m));
-            sn[m] = __builtin_bit_cast(f32x4, buf_load16_at(rs, off16, 1024 * m));
+            cs[w] = __builtin_bit_cast(f32x4, buf_load16_at(rc, off16, 2048 * half + 1024 * w));
+            sn[w] = __builtin_bit_cast(f32x4, buf_load16_at(rs, off16, 2048 * half + 1024 * w));
         }
     };
     float b_sum = 0.f;
-    // staging of one page in parts, spread over the 36 slots of a tile's two steps
+    // staging in parts, spread over the products of a tile's two steps
     struct Staging {
         uint32_t kd, vd, cd;
         float e, ks, inv;
         int ep;
         f32x4 vs;
         u32x2 ck[RTX];
-        f32x4 x, y, bx, by;
+        f32x4 x, y;
         u32x2 pk[2][2];  // [partner][tile of the quarter], packed
     };
-    const uint32_t bkt = lds0 + S::B_OFF + lane * 8;  // B_K^T fragments [rank tile][column tile][lane]
-    constexpr int PARTS = 30;
+    const uint32_t bkt = lds0 + S::B_OFF + half * 1024 + lane * 8;  // B_K^T fragments [rank tile][column tile][lane]
+    constexpr int PARTS = 18;
     auto low_rank = [&](const Staging &g, int m, f32x4 u) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < RT; ++t) u = mfma16(ld64(bkt + (t * 8 + m) * 512), g.ck[t], u);
         return u;
     };
     auto base_key = [&](const Staging &g, int m) __attribute__((always_inline)) {
-        const uint32_t w = kw[m / 4][m % 4];
+        const uint32_t w = kw[m / 4][m % 4];  // (tile m of the wave's: w or, its partner, 4 + w)
         const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, g.ks, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, g.ks, true);
         return f32x4{lo.x, lo.y, hi.x, hi.y};
     };
     auto stage_part = [&](Staging &g, int tile, auto part_tag) __attribute__((always_inline)) {
         constexpr int part = decltype(part_tag)::value;
-        if constexpr (part >= 5 && part <= 17 && part % 4 == 1) request_angles(tile, (part - 5) / 4);  // nine parts before their use
+        if constexpr (part == 2) request_angles(tile, 1);  // (tile 0: before the step)
         if constexpr (part == 0) {
             int lane = threadIdx.x & 63;
             asm("" : "+v"(lane));  // what follows from it is formed here, not kept for the launch
             const int col = lane & 15, grp = lane >> 4;
-            const int vis = L - (4 * tile + wave) * PS;  // tokens of the page inside the sequence
-            if (vis < PS) {  // unwritten values may be any bits, and meet zero weights
+            const int vis = L - (4 * tile + pw) * PS;  // tokens of the page inside the sequence
+            if (__builtin_expect(vis < PS, 0)) {  // unwritten values may be any bits, and meet zero weights
                 const int left = max(0, min(4, vis - 4 * grp));
                 const uint32_t m = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
                 ve &= m;
                 ke = col < vis ? ke : 0u;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) vw[j] = u32x4{vw[j].x & m, vw[j].y & m, vw[j].z & m, vw[j].w & m};
+                for (int j = 0; j < 2; ++j) vw[j] = u32x2{vw[j].x & m, vw[j].y & m};
                 if constexpr (R > 0) {
 #pragma unroll
                     for (int t = 0; t < RT; ++t) {
@@ -198,9 +194,9 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             // K: operand of step 2 kk + grp / 2, lane half grp % 2, row 16 (page % 2) + col; V, C_V: words of four tokens 4 grp .. + 3,
             // the lower or upper eight bytes of lane half grp % 2
             const uint32_t at = ((lane & 16) * 2 + (lane & 15)) * 16;  // of lane half grp % 2, row col
-            g.kd = lds0 + (tile & 1) * 16384 + (wave >> 1) * 8192 + (wave & 1) * 256 + (lane & 32) * 32 + at;
-            g.vd = lds0 + S::V_OFF + (tile % 3) * 16384 + wave * 4096 + (lane & 32) / 4 + at;
-            g.cd = g.vd + (S::C_OFF - S::V_OFF) + (tile % 3) * (S::C_TILE - 16384) + wave * (NRB * 1024 - 4096);
+            g.kd = lds0 + (tile & 1) * 16384 + (pw >> 1) * 8192 + (pw & 1) * 256 + half * 2048 + (lane & 32) * 32 + at;
+            g.vd = lds0 + S::V_OFF + (tile % 3) * 16384 + pw * 4096 + half * 1024 + (lane & 32) / 4 + at;
+            g.cd = g.vd + (S::C_OFF - S::V_OFF) + (tile % 3) * (S::C_TILE - 16384) + pw * (NRB * 1024 - 4096) - half * 1024;
             g.e = (float)((int)ke - 127 + 9);
             if constexpr (R > 0) {
                 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -218,67 +214,67 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
         } else if constexpr (part == 1) {
             g.ep = max(-100, min(126, (int)max_over_groups(max_over_row(g.e))));
         } else if constexpr (part == 2) {
-            if (lane == 0) page_exp[(tile & 1) * 4 + wave] = g.ep;
+            if (lane == 0) page_exp[(tile & 1) * 4 + pw] = g.ep;  // (both halves find the same)
             g.ks = __uint_as_float((uint32_t)max(0, min(254, (int)ke - g.ep)) << 23);
             g.inv = __uint_as_float((uint32_t)(127 - g.ep) << 23);
             g.vs = f32x4{f8_scale(ve & 255u), f8_scale((ve >> 8) & 255u), f8_scale((ve >> 16) & 255u), f8_scale(ve >> 24)};
-        } else if constexpr (part < 11) {
-            constexpr int i = part - 3;  // word i: dims 32 (i / 2) + 16 (i % 2) + col
-            const uint32_t w = vw[i / 4][i % 4];
+        } else if constexpr (part < 7) {
+            constexpr int i = part - 3;  // word i: dims 32 (half + 2 (i / 2)) + 16 (i % 2) + col
+            const uint32_t w = vw[i / 2][i % 2];
             const f32x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.f, true);
-            st64(g.vd + (i / 2) * 1024 + (i % 2) * 256, u32x2{pack_bf16(lo.x * g.vs.x, lo.y * g.vs.y), pack_bf16(hi.x * g.vs.z, hi.y * g.vs.w)});
-        } else if constexpr (part == 11) {
+            st64(g.vd + (i / 2) * 2048 + (i % 2) * 256, u32x2{pack_bf16(lo.x * g.vs.x, lo.y * g.vs.y), pack_bf16(hi.x * g.vs.z, hi.y * g.vs.w)});
+        } else if constexpr (part == 7) {
             if constexpr (R > 0) {
 #pragma unroll
                 for (int t = 0; t < RT; ++t) {
                     g.ck[t] = u32x2{pack_bf16(bf16_lo(c[t].x) * g.inv, bf16_hi(c[t].x) * g.inv), pack_bf16(bf16_lo(c[t].y) * g.inv, bf16_hi(c[t].y) * g.inv)};
-                    st64(g.cd + (t / 2) * 1024 + (t % 2) * 256, u32x2{c[t].z, c[t].w});
+                    if (half == 0) st64(g.cd + (t / 2) * 1024 + (t % 2) * 256, u32x2{c[t].z, c[t].w});
                 }
             }
-        } else if constexpr (part < 28) {
-            constexpr int i = (part - 12) / 4, s = (part - 12) % 4;  // tiles m and m + 4 (rotate-half partners), m = 2 kk + w
-            constexpr int m = i, kk = i / 2, w = i % 2;
+        } else if constexpr (part == 8) {
+            request(tile + 1);
+        } else if constexpr (part < 17) {
+            constexpr int w = (part - 9) / 4, s = (part - 9) % 4;  // the wave's tiles w and 4 + w (rotate-half partners)
             if constexpr (s == 0) {
                 if constexpr (R > 0) {
-                    g.x = low_rank(g, m, ROPE ? f32x4{0, 0, 0, 0} : base_key(g, m));
-                    g.y = low_rank(g, m + 4, ROPE ? f32x4{0, 0, 0, 0} : base_key(g, m + 4));
+                    g.x = low_rank(g, w, ROPE ? f32x4{0, 0, 0, 0} : base_key(g, w));
+                    g.y = low_rank(g, w + 4, ROPE ? f32x4{0, 0, 0, 0} : base_key(g, w + 4));
                 } else {
-                    g.x = base_key(g, m);
-                    g.y = base_key(g, m + 4);
+                    g.x = base_key(g, w);
+                    g.y = base_key(g, w + 4);
                 }
             } else if constexpr (s == 1) {
+                f32x4 x = g.x;
                 if constexpr (ROPE) {
-                    g.bx = base_key(g, m);
-                    g.by = base_key(g, m + 4);
-                }
-            } else if constexpr (s == 2) {
-                f32x4 x = g.x, y = g.y;
-                if constexpr (ROPE) {
+                    const f32x4 b = base_key(g, w);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[j] = __builtin_fmaf(g.x[j], cs[m][j], __builtin_fmaf(-g.y[j], sn[m][j], g.bx[j]));
-                        y[j] = __builtin_fmaf(g.y[j], cs[m][j], __builtin_fmaf(g.x[j], sn[m][j], g.by[j]));
-                    }
+                    for (int j = 0; j < 4; ++j) x[j] = __builtin_fmaf(g.x[j], cs[w][j], __builtin_fmaf(-g.y[j], sn[w][j], b[j]));
                 }
                 g.pk[0][w] = u32x2{pack_f16(x.x, x.y), pack_f16(x.z, x.w)};
+            } else if constexpr (s == 2) {
+                f32x4 y = g.y;
+                if constexpr (ROPE) {
+                    const f32x4 b = base_key(g, w + 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y[j] = __builtin_fmaf(g.y[j], cs[w][j], __builtin_fmaf(g.x[j], sn[w][j], b[j]));
+                }
                 g.pk[1][w] = u32x2{pack_f16(y.x, y.y), pack_f16(y.z, y.w)};
             } else if constexpr (w == 1) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j) st128(g.kd + (kk + 2 * j) * 2048, u32x4{g.pk[j][0].x, g.pk[j][0].y, g.pk[j][1].x, g.pk[j][1].y});
+                for (int j = 0; j < 2; ++j) st128(g.kd + j * 4096, u32x4{g.pk[j][0].x, g.pk[j][0].y, g.pk[j][1].x, g.pk[j][1].y});
             }
-        } else if constexpr (part == 28) {
-            request(tile + 1);
+        } else if constexpr (part == 17) {
+            request_keys(tile + 1);
         }
     };
 
     // ---- queries (B operand: lane = row, dims 32 kk + 4 g + 0..3 and 16 further, g = 2 (st % 2) + hh), fp16 times 2^-eq ----
-    int row_tok[2], eq[2];
-    u32x4 qf[2][8];
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-        const int rr = wave * 64 + rb * 32 + r32, tk = tok_begin + rr / G;
+    int row_tok, eq;
+    u32x4 qf[8];
+    {
+        const int rr = wave * 32 + r32, tk = tok_begin + rr / G;
         const bool ok = tk < nq;
-        row_tok[rb] = ok ? tk : -1;
+        row_tok = ok ? tk : -1;
         const uint16_t *qr = p.q + ((int64_t)(q0 + (ok ? tk : 0)) * p.hq + h * G + rr % G) * D;
         float big = 0.f;
 #pragma unroll
@@ -291,20 +287,17 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) big = fmaxf(big, fmaxf(fabsf(bf16_lo(v[i])), fabsf(bf16_hi(v[i]))));
-            qf[rb][st] = v;
+            qf[st] = v;
         }
-        eq[rb] = max(-100, min(126, (int)(__float_as_uint(max_over_halves(big)) >> 23) - 126));
-        const float inv = __uint_as_float((uint32_t)(127 - eq[rb]) << 23);
+        eq = max(-100, min(126, (int)(__float_as_uint(max_over_halves(big)) >> 23) - 126));
+        const float inv = __uint_as_float((uint32_t)(127 - eq) << 23);
 #pragma unroll
         for (int st = 0; st < 8; ++st)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) qf[rb][st][i] = pack_f16(bf16_lo(qf[rb][st][i]) * inv, bf16_hi(qf[rb][st][i]) * inv);
-        if (rb == 0 || NRB < 2) {  // from here on in accumulation registers
-#pragma unroll
-            for (int st = 0; st < 8; ++st) asm("" : "+a"(qf[rb][st]));
-        }
+            for (int i = 0; i < 4; ++i) qf[st][i] = pack_f16(bf16_lo(qf[st][i]) * inv, bf16_hi(qf[st][i]) * inv);
     }
     request(0);
+    request_keys(0);
     if constexpr (R > 0) {
         // B_K^T fragments: lane (c, g) of (tile t, column tile m) holds B_K[16t + 4g + 0..3][16m + c]; sums of the ranks' largest
         const uint16_t *bk = p.lora_b + (int64_t)ad * 2 * R * n + (int64_t)h * D;
@@ -337,30 +330,36 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
         __syncthreads();
     }
 
-    f32x16 oacc[4][2], racc[NRBX][2];
+    f32x16 oacc[4], racc[NRBX], s;  // s: scores of 32 keys
 #pragma unroll
-    for (int b = 0; b < 4; ++b) oacc[b][0] = oacc[b][1] = f32x16{};
+    for (int b = 0; b < 4; ++b) oacc[b] = f32x16{};
 #pragma unroll
-    for (int b = 0; b < NRBX; ++b) racc[b][0] = racc[b][1] = f32x16{};
-    f32x16 s[2];  // scores of 32 keys
-    float m_run[2] = {kNegInf, kNegInf}, lsum[2] = {0.f, 0.f};
+    for (int b = 0; b < NRBX; ++b) racc[b] = f32x16{};
+    float m_run = kNegInf, lsum = 0.f;
     const float cl = p.scale_log2;
 
     // One step: PV: values of block pv_kb of tile pv_tile with the weights pf_in, beside (EXP) the weights of the scores s (32 keys from
-    // key0; page exponents at pe) into pf_out; then QK: scores of block qk_kb of tile qk_tile into s, beside (STAGE) the first or second
+    // key0; page exponents e0, e1) into pf_out; then QK: scores of block qk_kb of tile qk_tile into s, beside (STAGE) the first or second
     // half of the staging of tile st_tile.
-    constexpr int NP = 8 + 2 * NRB;
-    auto step = [&](auto exp_tag, auto qk_tag, auto pv_tag, auto stage_tag, u32x4 (&pf_in)[2][2], u32x4 (&pf_out)[2][2], int key0, int pe, int qk_tile,
-                    int qk_kb, int pv_tile, int pv_kb, Staging &g, int st_tile) __attribute__((always_inline)) {
+    constexpr int NP = 8 + 2 * NRB, SLOTS = NP + 8, PRE = 2;  // products of the values, of a step; operands read ahead (four
+    // spill at ranks over 16: 639 TFLOP/s at rank 64, not 700)
+    u32x4 ahead[PRE];
+    auto step = [&](auto exp_tag, auto qk_tag, auto pv_tag, auto stage_tag, u32x4 (&pf_in)[2], u32x4 (&pf_out)[2], int key0, int e0, int e1, int qk_tile,
+                    int qk_kb, int pv_tile, int pv_kb, int next_tile, int next_kb, Staging &g, int st_tile) __attribute__((always_inline)) {
         constexpr bool EXP = decltype(exp_tag)::value, QK = decltype(qk_tag)::value, PV = decltype(pv_tag)::value;
         constexpr int STAGE = decltype(stage_tag)::value;  // 0: none, 1: first half of the parts, 2: second half
         const uint32_t ka = lds0 + (qk_tile & 1) * 16384 + qk_kb * 8192 + lane * 16;
         const uint32_t va = lds0 + S::V_OFF + (pv_tile % 3) * 16384 + pv_kb * 8192 + lane * 16;
         const uint32_t ca = lds0 + S::C_OFF + (pv_tile % 3) * S::C_TILE + pv_kb * 2 * NRB * 1024 + lane * 16;
-        // product slots: those of the values (page i / (4 + NRB), block i % (4 + NRB)), then those of the scores
+        const uint32_t vn = lds0 + S::V_OFF + (next_tile % 3) * 16384 + next_kb * 8192 + lane * 16;
+        const uint32_t cn = lds0 + S::C_OFF + (next_tile % 3) * S::C_TILE + next_kb * 2 * NRB * 1024 + lane * 16;
+        // operands in order: those of the values (page i / (4 + NRB), block i % (4 + NRB)), of the scores, then the next step's first
         auto frag = [&](auto slot_tag) __attribute__((always_inline)) -> u32x4 {
             constexpr int slot = decltype(slot_tag)::value;
-            if constexpr (slot >= NP) {
+            if constexpr (slot >= SLOTS) {
+                constexpr int pg = (slot - SLOTS) / (4 + NRB), b = (slot - SLOTS) % (4 + NRB);
+                return b < 4 ? lds_load(vn + pg * 4096 + b * 1024) : lds_load(cn + (pg * NRB + b - 4) * 1024);
+            } else if constexpr (slot >= NP) {
                 return QK ? lds_load(ka + (slot - NP) * 1024) : u32x4{};
             } else {
                 constexpr int pg = slot / (4 + NRB), b = slot % (4 + NRB);
@@ -368,119 +367,92 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
                 return b < 4 ? lds_load(va + pg * 4096 + b * 1024) : lds_load(ca + (pg * NRB + b - 4) * 1024);
             }
         };
-        auto product = [&](auto slot_tag, auto rb_tag, const u32x4 &f) __attribute__((always_inline)) {
-            constexpr int slot = decltype(slot_tag)::value, rb = decltype(rb_tag)::value;
+        auto product = [&](auto slot_tag, const u32x4 &f) __attribute__((always_inline)) {
+            constexpr int slot = decltype(slot_tag)::value;
             if constexpr (slot >= NP) {
                 constexpr int i = slot - NP;
-                if constexpr (QK) score_product<i == 0, (rb == 0 || NRB < 2)>(s[rb], f, qf[rb][i]);
+                if constexpr (QK) s = mfma32x32_f16(f, qf[i], i == 0 ? f32x16{} : s);
             } else if constexpr (PV) {
                 constexpr int pg = slot / (4 + NRB), b = slot % (4 + NRB);
-                if constexpr (b < 4) oacc[b][rb] = mfma32x32(f, pf_in[pg][rb], oacc[b][rb]);
-                else racc[b - 4][rb] = mfma32x32(f, pf_in[pg][rb], racc[b - 4][rb]);
+                if constexpr (b < 4) oacc[b] = mfma32x32(f, pf_in[pg], oacc[b]);
+                else racc[b - 4] = mfma32x32(f, pf_in[pg], racc[b - 4]);
             }
         };
-        float f[2][2], mx[2], alpha[2], tsum[2] = {0.f, 0.f};  // f [page][row block]
+        float f[2], mx, alpha, tsum = 0.f;  // f [page]
         bool moved = false;
         if constexpr (EXP) {
-            score_wait(s);
-            const int e0 = page_exp[pe], e1 = page_exp[pe + 1];
-            if (key0 + 31 > P0 + tok_begin) {  // causal mask
+            if (__builtin_expect(key0 + 31 > P0 + tok_begin, 0)) {  // causal mask
+                const int lim = row_tok < 0 ? -1 : P0 + row_tok - key0 - 4 * hh;
 #pragma unroll
-                for (int rb = 0; rb < 2; ++rb) {
-                    const int lim = row_tok[rb] < 0 ? -1 : P0 + row_tok[rb] - key0 - 4 * hh;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[rb][i] = 8 * (i / 4) + i % 4 <= lim ? s[rb][i] : kNegInf;
-                }
-            }
-#pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {  // neither 0 nor infinite: masked scores and zeros stay
-                f[0][rb] = fminf(fmaxf(ldexpf(cl, e0 + eq[rb]), 1.2e-38f), 3e38f);
-                f[1][rb] = fminf(fmaxf(ldexpf(cl, e1 + eq[rb]), 1.2e-38f), 3e38f);
+                for (int i = 0; i < 16; ++i) s[i] = 8 * (i / 4) + i % 4 <= lim ? s[i] : kNegInf;
             }
         }
-        auto maxima = [&](int rb) __attribute__((always_inline)) {
-            float x0 = max3(s[rb][0], s[rb][1], s[rb][2]), x1 = max3(s[rb][8], s[rb][9], s[rb][10]);
-            x0 = max3(x0, s[rb][3], s[rb][4]);
-            x1 = max3(x1, s[rb][11], s[rb][12]);
-            x0 = max3(x0, max3(s[rb][5], s[rb][6], s[rb][7]), x0);
-            x1 = max3(x1, max3(s[rb][13], s[rb][14], s[rb][15]), x1);
-            mx[rb] = max_over_halves(fmaxf(x0 * f[0][rb], x1 * f[1][rb]));
-        };
-        auto weights = [&](auto pair_tag) __attribute__((always_inline)) {  // pair w of 16: row block w / 8, values 2 (w % 8), + 1
-            constexpr int w = decltype(pair_tag)::value, rb = w / 8, i = 2 * (w % 8), pg = i / 8;
-            const float m_use = m_run[rb] == kNegInf ? 0.f : m_run[rb];
-            const float e0 = fast_exp2(__builtin_fmaf(s[rb][i], f[pg][rb], -m_use)), e1 = fast_exp2(__builtin_fmaf(s[rb][i + 1], f[pg][rb], -m_use));
-            uint32_t pk = pack_bf16(e0, e1);
-            asm volatile("" : "+v"(pk));  // stays here: otherwise the compiler moves the weights past the branch below, behind the products
-            pf_out[pg][rb][(i % 8) / 2] = pk;
-            if constexpr (!LROW) tsum[rb] = add_bf16_pair(pk, tsum[rb]);  // the weights as the products take them: their rounding cancels in O / l
-        };
-        // beside product i (two per operand, so that vector work fills the time of each: a wave that issues two products in a row
-        // stands still for the length of the first)
-        constexpr int PRE = 4, SLOTS = NP + 8, FIRST = 4;  // operands read ahead; first product with weights beside it
-        auto beside = [&](auto product_tag) __attribute__((always_inline)) {
-            constexpr int i = decltype(product_tag)::value;
-            if constexpr (EXP && i < 2 * NP) {
-                if constexpr (i == 1) maxima(0);
-                if constexpr (i == 2) maxima(1);
-                if constexpr (i == 3) {
-                    const float up = fmaxf(mx[0] - m_run[0], mx[1] - m_run[1]);  // (NaN for a row that has seen no key: -inf - -inf)
-                    moved = __builtin_amdgcn_ballot_w64(up > kLazyRescale) != 0;
-                    if (moved) {
+        auto maxima = [&]() __attribute__((always_inline)) {
+            f[0] = fminf(fmaxf(ldexpf(cl, e0 + eq), 1.2e-38f), 3e38f);  // neither 0 nor infinite: masked scores and zeros stay
+            f[1] = fminf(fmaxf(ldexpf(cl, e1 + eq), 1.2e-38f), 3e38f);
+            float x0 = fmaxf(s[0], s[1]), x1 = fmaxf(s[8], s[9]);
 #pragma unroll
-                        for (int rb = 0; rb < 2; ++rb) {
-                            const float m_new = fmaxf(m_run[rb], mx[rb]);
-                            alpha[rb] = fast_exp2(m_run[rb] - (m_new == kNegInf ? 0.f : m_new));
-                            m_run[rb] = m_new;
-                        }
+            for (int i = 2; i < 8; i += 2) {
+                x0 = fmaxf(fmaxf(x0, s[i]), s[i + 1]);
+                x1 = fmaxf(fmaxf(x1, s[8 + i]), s[9 + i]);
+            }
+            mx = fmaxf(x0 * f[0], x1 * f[1]);
+        };
+        auto weights = [&](auto pair_tag) __attribute__((always_inline)) {  // values 2 w, 2 w + 1 of the lane's 16
+            constexpr int w = decltype(pair_tag)::value, i = 2 * w, pg = i / 8;
+            const float m_use = m_run == kNegInf ? 0.f : m_run;
+            const float w0 = fast_exp2(__builtin_fmaf(s[i], f[pg], -m_use)), w1 = fast_exp2(__builtin_fmaf(s[i + 1], f[pg], -m_use));
+            uint32_t pk = pack_bf16(w0, w1);
+            asm volatile("" : "+v"(pk));  // stays here: otherwise the compiler moves the weights past the branch below, behind the products
+            pf_out[pg][(i % 8) / 2] = pk;
+            if constexpr (!LROW) tsum = add_bf16_pair(pk, tsum);  // the weights as the products take them: their rounding cancels in O / l
+        };
+        auto beside = [&](auto slot_tag) __attribute__((always_inline)) {
+            constexpr int i = decltype(slot_tag)::value, FIRST = 2;
+            if constexpr (EXP && i < NP) {
+                if constexpr (i == 0) maxima();
+                if constexpr (i == 1) {
+                    mx = max_over_halves(mx);
+                    moved = __builtin_amdgcn_ballot_w64(mx > m_run + kLazyRescale) != 0;
+                    if (__builtin_expect(moved, 0)) {
+                        const float m_new = fmaxf(m_run, mx);
+                        alpha = fast_exp2(m_run - (m_new == kNegInf ? 0.f : m_new));
+                        m_run = m_new;
                     }
                 }
                 if constexpr (i >= FIRST) {
-                    constexpr int n = 2 * NP - FIRST, w0 = 16 * (i - FIRST) / n, w1 = 16 * (i + 1 - FIRST) / n;
-                    each<w1 - w0>([&](auto q) __attribute__((always_inline)) { weights(std::integral_constant<int, w0 + q.value>{}); });
+                    constexpr int n = NP - FIRST, a0 = 8 * (i - FIRST) / n, a1 = 8 * (i + 1 - FIRST) / n;
+                    each<a1 - a0>([&](auto q) __attribute__((always_inline)) { weights(std::integral_constant<int, a0 + q.value>{}); });
                 }
-                if constexpr (i == 2 * NP - 1) {
-                    if (moved) {
+                if constexpr (i == NP - 1) {
+                    if (__builtin_expect(moved, 0)) {
 #pragma unroll
-                        for (int rb = 0; rb < 2; ++rb) {
+                        for (int b = 0; b < 4; ++b) oacc[b] *= alpha;
 #pragma unroll
-                            for (int b = 0; b < 4; ++b) {  // (one block at a time: they come to vector registers for it)
-                                oacc[b][rb] *= alpha[rb];
-                                fence();
-                            }
-#pragma unroll
-                            for (int b = 0; b < NRB; ++b) {
-                                racc[b][rb] *= alpha[rb];
-                                fence();
-                            }
-                            lsum[rb] *= alpha[rb];
-                        }
+                        for (int b = 0; b < NRB; ++b) racc[b] *= alpha;
+                        lsum *= alpha;
                     }
-                    if constexpr (!LROW) {
-                        lsum[0] += tsum[0];
-                        lsum[1] += tsum[1];
-                    }
+                    if constexpr (!LROW) lsum += tsum;
                 }
             }
-            if constexpr (STAGE > 0 && i >= 2 * NP) {
-                constexpr int HALF = PARTS / 2, q = i - 2 * NP, p0 = HALF * q / 16, p1 = HALF * (q + 1) / 16;
+            if constexpr (STAGE > 0 && i >= NP) {
+                constexpr int HALF = PARTS / 2, q = i - NP, p0 = HALF * q / 8, p1 = HALF * (q + 1) / 8;
                 each<p1 - p0>([&](auto k) __attribute__((always_inline)) {
                     stage_part(g, st_tile, std::integral_constant<int, (STAGE - 1) * HALF + p0 + k.value>{});
                 });
             }
             fence();
         };
-        u32x4 fr[PRE];
-        each<PRE>([&](auto q) __attribute__((always_inline)) { fr[q.value] = frag(q); });
+        u32x4 fr[SLOTS + PRE];
+        each<PRE>([&](auto q) __attribute__((always_inline)) { fr[q.value] = ahead[q.value]; });
         fence();
         each<SLOTS>([&](auto slot_tag) __attribute__((always_inline)) {
             constexpr int slot = decltype(slot_tag)::value;
-            product(slot_tag, std::integral_constant<int, 0>{}, fr[slot % PRE]);
-            beside(std::integral_constant<int, 2 * slot>{});
-            product(slot_tag, std::integral_constant<int, 1>{}, fr[slot % PRE]);
-            if constexpr (slot + PRE < SLOTS) fr[slot % PRE] = frag(std::integral_constant<int, slot + PRE>{});
-            beside(std::integral_constant<int, 2 * slot + 1>{});
+            product(slot_tag, fr[slot]);
+            fr[slot + PRE] = frag(std::integral_constant<int, slot + PRE>{});
+            beside(slot_tag);
         });
+        each<PRE>([&](auto q) __attribute__((always_inline)) { ahead[q.value] = fr[SLOTS + q.value]; });
     };
     using T = std::true_type;
     using F = std::false_type;
@@ -488,27 +460,32 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     using N1 = std::integral_constant<int, 1>;
     using N2 = std::integral_constant<int, 2>;
     Staging g;
-    u32x4 pa[2][2], pb[2][2];  // weights of a tile's second and first half [page][row block]
+    u32x4 pa[2], pb[2];  // weights of a tile's second and first half [page]
 
+    request_angles(0, 0);
     each<PARTS>([&](auto i) __attribute__((always_inline)) { stage_part(g, 0, i); });  // (requests tile 1)
     __syncthreads();
     // tile 0: no values yet
-    step(F{}, T{}, F{}, N1{}, pa, pb, 0, 0, 0, 0, 0, 0, g, 1);
-    step(T{}, T{}, F{}, N2{}, pa, pb, 0, 0, 0, 1, 0, 0, g, 1);
+    auto exps_of = [&](int tile) __attribute__((always_inline)) { return *reinterpret_cast<const i32x4 *>(page_exp + (tile & 1) * 4); };
+    i32x4 e = exps_of(0);
+    request_angles(1, 0);
+    step(F{}, T{}, F{}, N1{}, pa, pb, 0, 0, 0, 0, 0, 0, 0, 0, 0, g, 1);
+    step(T{}, T{}, F{}, N2{}, pa, pb, 0, e.x, e.y, 0, 1, 0, 0, 0, 0, g, 1);
     for (int u = 1; u < n_tiles; ++u) {
-        __syncthreads();  // tile u is staged, tile u - 1's keys and tile u - 2's values are read
-        step(T{}, T{}, T{}, N1{}, pb, pa, (u - 1) * TILE_KEYS + 32, ((u - 1) & 1) * 4 + 2, u, 0, u - 1, 0, g, u + 1);
-        step(T{}, T{}, T{}, N2{}, pa, pb, u * TILE_KEYS, (u & 1) * 4, u, 1, u - 1, 1, g, u + 1);
+        lds_fence_barrier();  // (not one that waits for the loads in flight) tile u is staged, tile u - 1's keys and tile u - 2's values are read
+        const i32x4 en = exps_of(u);
+        request_angles(u + 1, 0);
+        step(T{}, T{}, T{}, N1{}, pb, pa, (u - 1) * TILE_KEYS + 32, e.z, e.w, u, 0, u - 1, 0, u - 1, 1, g, u + 1);
+        step(T{}, T{}, T{}, N2{}, pa, pb, u * TILE_KEYS, en.x, en.y, u, 1, u - 1, 1, u, 0, g, u + 1);
+        e = en;
     }
     // the last tile's second half, and its values
-    step(T{}, F{}, T{}, N0{}, pb, pa, (n_tiles - 1) * TILE_KEYS + 32, ((n_tiles - 1) & 1) * 4 + 2, 0, 0, n_tiles - 1, 0, g, 0);
-    step(F{}, F{}, T{}, N0{}, pa, pb, 0, 0, 0, 0, n_tiles - 1, 1, g, 0);
+    step(T{}, F{}, T{}, N0{}, pb, pa, (n_tiles - 1) * TILE_KEYS + 32, e.z, e.w, 0, 0, n_tiles - 1, 0, n_tiles - 1, 1, g, 0);
+    step(F{}, F{}, T{}, N0{}, pa, pb, 0, 0, 0, 0, 0, n_tiles - 1, 1, 0, 0, g, 0);
     __syncthreads();
 
     // ---- epilogue: O = (acc + acc_r . B_V[h]) / l; lane: row r32, dims 32 b + 8 (i / 4) + 4 hh + i % 4 ----
-    float l_run[2];
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) l_run[rb] = LROW ? racc[0][rb][8] : lsum[rb] + __shfl_xor(lsum[rb], 32);
+    const float l_run = LROW ? __shfl(racc[0][8], r32) : lsum + __shfl_xor(lsum, 32);
     if constexpr (R > 0) {
         float *bv = reinterpret_cast<float *>(lds), *acc = bv + R * D;
         const uint16_t *src = p.lora_b + ((int64_t)ad * 2 + 1) * R * n + (int64_t)h * D;
@@ -518,41 +495,34 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             bv[2 * e + 1] = bf16_hi(w);
         }
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
+        for (int b = 0; b < NRB; ++b)
 #pragma unroll
-            for (int b = 0; b < NRB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int rho = 32 * b + 8 * (i / 4) + 4 * hh + i % 4;
-                    if (rho < R) acc[(wave * 64 + rb * 32 + r32) * (R + 1) + rho] = racc[b][rb][i];
-                }
+            for (int i = 0; i < 16; ++i) {
+                const int rho = 32 * b + 8 * (i / 4) + 4 * hh + i % 4;
+                if (rho < R) acc[(wave * 32 + r32) * (R + 1) + rho] = racc[b][i];
+            }
         __syncthreads();
 #pragma unroll 2
         for (int rho = 0; rho < R; ++rho) {
-            const float x0 = acc[(wave * 64 + r32) * (R + 1) + rho], x1 = acc[(wave * 64 + 32 + r32) * (R + 1) + rho];
+            const float x = acc[(wave * 32 + r32) * (R + 1) + rho];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const f32x4 v = *reinterpret_cast<const f32x4 *>(bv + rho * D + 32 * b + 8 * i + 4 * hh);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        oacc[b][0][4 * i + j] += x0 * v[j];
-                        oacc[b][1][4 * i + j] += x1 * v[j];
-                    }
+                    for (int j = 0; j < 4; ++j) oacc[b][4 * i + j] += x * v[j];
                 }
         }
     }
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-        if (row_tok[rb] < 0) continue;
-        const float inv = l_run[rb] > 0.f ? 1.f / l_run[rb] : 0.f;
-        uint16_t *o = p.out + ((int64_t)(q0 + row_tok[rb]) * p.hq + h * G + (wave * 64 + rb * 32 + r32) % G) * D;
+    if (row_tok >= 0) {
+        const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+        uint16_t *o = p.out + ((int64_t)(q0 + row_tok) * p.hq + h * G + (wave * 32 + r32) % G) * D;
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const f32x4 v = {oacc[b][rb][4 * i] * inv, oacc[b][rb][4 * i + 1] * inv, oacc[b][rb][4 * i + 2] * inv, oacc[b][rb][4 * i + 3] * inv};
+                const f32x4 v = {oacc[b][4 * i] * inv, oacc[b][4 * i + 1] * inv, oacc[b][4 * i + 2] * inv, oacc[b][4 * i + 3] * inv};
                 *reinterpret_cast<u32x2 *>(o + 32 * b + 8 * i + 4 * hh) = pack4(v);
             }
     }
