@@ -40,7 +40,7 @@ hipError_t launch_stream(int r, int g, bool rope, bool rows128, const PrefillArg
 // Launch of the kernels over 8-bit base pages (prefill_fp8.hip), which sets blocks_per_agent_head for chunks of up to max_q tokens.
 hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev);
 
-// The one of large grids (prefill_fp8_stream.hip): 256 query rows per workgroup.
-hipError_t launch_fp8_stream(int r, int g, const PrefillArgs &pa, hipStream_t st, void *const *ev);
+// The one of all but small grids (prefill_fp8_stream.hip): 256 or 128 query rows per workgroup.
+hipError_t launch_fp8_stream(int r, int g, int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev);
 
 }  // namespace fkvp

@@ -8,7 +8,7 @@
 //               K = K_base + RoPE_p(B_K^T C_K^T) (without tables no rotation), V = code * 2^E.
 //   every wave  S^T = K Q^T, causal mask + online softmax, O^T += V^T P^T, acc_r^T += C_V^T P^T over its 8 NRG / 8 pages
 // and at the end the key groups' rows are merged and O = (O + acc_r . B_V[h]) / l (Eq. 4) is written in bf16.  This is the kernel of
-// workgroups of 128, 64 and 32 rows, where 256 would leave compute units idle; prefill_fp8_stream.hip has the one of 256.
+// workgroups of 64 and 32 rows, where more would leave compute units idle; prefill_fp8_stream.hip has the one of 256 and 128.
 //
 // K and Q are fp16 here, 11 significant bits: the sum of a base key, exact in four bits, and its low-rank part would
 // lose what bf16 keeps of it alone (error of the result 5.6e-3 with bf16 keys at 8B heads, rank 16, over 9000 tokens, 2-norm; 2.2e-3 in
@@ -488,8 +488,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
 }
 
 // Rows per workgroup: the most (of 256, 128, 64, 32) whose workgroups still fill every compute unit of the fullest XCD (an (agent,
-// KV head) pair keeps to one XCD), else 32.  Four chunks of up to 250 tokens over 35k, 8B heads: 128 rows 1019 us, 256 rows 1214 us;
-// eight of up to 1024 over 9.5k, RoPE: 256 rows 1698 us, 128 rows 2168 us.
+// KV head) pair keeps to one XCD), else 32.  Four chunks of up to 250 tokens over 35k, 8B heads: 128 rows 939 us, 256 rows 1214 us;
+// eight of up to 1024 over 9.5k, RoPE: 256 rows 1664 us, 128 rows 2168 us (this file's kernel).
 int rows_of(int64_t pairs, int64_t max_q, int g) {
     const int64_t per_xcd = (pairs + kXcds - 1) / kXcds;
     for (int rows = 256; rows > 32; rows /= 2)
@@ -509,7 +509,6 @@ hipError_t launch(const PrefillArgs &pa, hipStream_t st, void *const *ev) {
 template <int R, int G>
 hipError_t dispatch_rows(int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     switch (rows) {
-    case 128: return launch<R, G, 4>(pa, st, ev);
     case 64: return launch<R, G, 2>(pa, st, ev);
     default: return launch<R, G, 1>(pa, st, ev);
     }
@@ -532,7 +531,7 @@ hipError_t dispatch(int r, int rows, const PrefillArgs &pa, hipStream_t st, void
 hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev) {
     const int rows = rows_of((int64_t)pa.n_agents * pa.hkv, max_q, g);
     pa.blocks_per_agent_head = (int)((max_q * g + rows - 1) / rows);
-    if (rows == 256) return launch_fp8_stream(r, g, pa, st, ev);  // (measured beside that kernel)
+    if (rows >= 128) return launch_fp8_stream(r, g, rows, pa, st, ev);  // (measured beside that kernel)
     return g == 4 ? dispatch<4>(r, rows, pa, st, ev) : dispatch<8>(r, rows, pa, st, ev);
 }
 

@@ -1,7 +1,7 @@
-// ResidualAttention chunked prefill over 8-bit base pages, the kernel of large grids (Section 6 prefill kernel, Algorithm 1 with
-// a block of query rows; fp8_cache.hpp has the page format, prefill_fp8.hip the scales of K and Q and the kernel of small grids).
+// ResidualAttention chunked prefill over 8-bit base pages, the kernel of all but small grids (Section 6 prefill kernel, Algorithm 1 with
+// a block of query rows; fp8_cache.hpp has the page format, prefill_fp8.hip the scales of K and Q and that of small grids).
 //
-// One workgroup of eight waves = (agent a, KV head h, block of 256 query rows), 32 rows per wave and two waves per SIMD (within 256
+// One workgroup of eight waves = (agent a, KV head h, block of 256 query rows), one row group of 32 rows per wave and two waves per SIMD (within 256
 // registers each): while one wave's products hold the matrix cores the other issues its vector work.  Four waves of 64 rows read
 // half as much from LDS (every operand serves two products) and were slower, 895 against 920 TFLOP/s without adapters, 733 against 752
 // at rank 16 with RoPE and 300 against 700 at rank 64, where their accumulators spilled: alone on its SIMD, a wave's vector instructions
@@ -19,6 +19,11 @@
 // Measured at 16 chunks of 1024 tokens over 9.5k tokens of context, 8B heads: 950 TFLOP/s without adapters (a large bf16 product of
 // the library: 1140), 905 with rank 16 (prefill_fp8.hip's kernel at 256 rows: 823), 757 with RoPE (712), and 700 at rank 64 with RoPE
 // over 70B heads (511).
+//
+// Where 256 rows leave compute units idle a workgroup has 128 rows in four row groups, and two key groups of four waves take one half
+// of every tile each: one step per tile, beside all of its staging, with the values two tiles behind the scores; at the end the second
+// group's rows are merged into the first's.  Four chunks of up to 250 tokens, 8B heads: rank 16 over 35k 939 us (prefill_fp8.hip's kernel
+// at 128 rows: 1028), over 17k without adapters 415 (418), rank 32 with RoPE 592 (650), rank 64 with RoPE 869 (941) and without 625 (868).
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
@@ -36,18 +41,21 @@ using namespace fkvk;
 namespace fkvp {
 namespace {
 
-constexpr int D = 128, PS = 16, TILE_KEYS = 64, WAVES = 8, ROWS = 256;
+constexpr int D = 128, PS = 16, TILE_KEYS = 64, WAVES = 8;
 constexpr float kNegInf = -INFINITY, kLazyRescale = 8.f;
 
-template <int R>
+template <int R, int KG>
 struct Lay {
+    static constexpr int ROWS = 32 * WAVES / KG, VT = KG == 1 ? 3 : 4;  // query rows; tiles of V and C_V kept
     static constexpr int RT = R == 0 ? 0 : (R + 15) / 16, NRB = (RT + 1) / 2;
     static constexpr bool LROW = RT == 1;  // rows 16..31 of the rank block are ones: the row sums come with acc_r
-    // K [2 tiles][32-key block][step][lane] 16 B, V [3 tiles][page][32-dim block][lane] 16 B, C_V [3 tiles][page][32-rank block][lane] 16 B
-    static constexpr int V_OFF = 2 * 16384, C_OFF = V_OFF + 3 * 16384, C_TILE = 4 * NRB * 1024;
-    static constexpr int B_OFF = C_OFF + 3 * C_TILE, E_OFF = B_OFF + RT * 4096, MAIN = E_OFF + 64;
+    // K [2 tiles][32-key block][step][lane] 16 B, V [VT tiles][page][32-dim block][lane] 16 B, C_V [VT tiles][page][32-rank block][lane] 16 B
+    static constexpr int V_OFF = 2 * 16384, C_OFF = V_OFF + VT * 16384, C_TILE = 4 * NRB * 1024;
+    static constexpr int B_OFF = C_OFF + VT * C_TILE, E_OFF = B_OFF + RT * 4096, MAIN = E_OFF + 64;
     static constexpr int EPI = R * D * 4 + ROWS * (R + 1) * 4;
+    static constexpr int NF4 = 16 + 4 * (NRB > 0 ? NRB : 1) + 1;  // a wave's rows: oacc, racc, (m, l)
     static constexpr int BYTES = MAIN > EPI ? MAIN : EPI;
+    static_assert(KG == 1 || WAVES / 2 * NF4 * 1024 <= BYTES, "merge area");
     static_assert(BYTES <= 160 * 1024, "LDS of one workgroup");
 };
 
@@ -71,13 +79,14 @@ __device__ __forceinline__ void each(F &&f) {
 }
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
-template <int R, int G, bool ROPE>
+template <int R, int G, bool ROPE, int KG>
 __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, int a, int h, int tok_begin) {
-    using S = Lay<R>;
-    constexpr int RT = S::RT, RTX = RT > 0 ? RT : 1, NRB = S::NRB, NRBX = NRB > 0 ? NRB : 1, TPW = ROWS / G;
+    using S = Lay<R, KG>;
+    constexpr int RT = S::RT, RTX = RT > 0 ? RT : 1, NRB = S::NRB, NRBX = NRB > 0 ? NRB : 1, TPW = S::ROWS / G, VT = S::VT;
     constexpr bool LROW = S::LROW;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const int col = lane & 15, grp = lane >> 4, hh = lane >> 5, r32 = lane & 31;
+    const int rg = wave % (WAVES / KG), kg = wave / (WAVES / KG);  // row group, key group
     const int hkv = p.hkv;
     const int64_t n = (int64_t)hkv * D;
     const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
@@ -195,8 +204,8 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             // the lower or upper eight bytes of lane half grp % 2
             const uint32_t at = ((lane & 16) * 2 + (lane & 15)) * 16;  // of lane half grp % 2, row col
             g.kd = lds0 + (tile & 1) * 16384 + (pw >> 1) * 8192 + (pw & 1) * 256 + half * 2048 + (lane & 32) * 32 + at;
-            g.vd = lds0 + S::V_OFF + (tile % 3) * 16384 + pw * 4096 + half * 1024 + (lane & 32) / 4 + at;
-            g.cd = g.vd + (S::C_OFF - S::V_OFF) + (tile % 3) * (S::C_TILE - 16384) + pw * (NRB * 1024 - 4096) - half * 1024;
+            g.vd = lds0 + S::V_OFF + (tile % VT) * 16384 + pw * 4096 + half * 1024 + (lane & 32) / 4 + at;
+            g.cd = g.vd + (S::C_OFF - S::V_OFF) + (tile % VT) * (S::C_TILE - 16384) + pw * (NRB * 1024 - 4096) - half * 1024;
             g.e = (float)((int)ke - 127 + 9);
             if constexpr (R > 0) {
                 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
@@ -272,7 +281,7 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     int row_tok, eq;
     u32x4 qf[8];
     {
-        const int rr = wave * 32 + r32, tk = tok_begin + rr / G;
+        const int rr = rg * 32 + r32, tk = tok_begin + rr / G;
         const bool ok = tk < nq;
         row_tok = ok ? tk : -1;
         const uint16_t *qr = p.q + ((int64_t)(q0 + (ok ? tk : 0)) * p.hq + h * G + rr % G) * D;
@@ -321,7 +330,7 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             st64(lds0 + S::B_OFF + idx * 8, u32x2{w[0], w[1]});
         }
         if constexpr (LROW) {  // rows 16..31 of the rank block: ones, for the launch
-            for (int idx = threadIdx.x; idx < 3 * 4 * 64; idx += 64 * WAVES)
+            for (int idx = threadIdx.x; idx < VT * 4 * 64; idx += 64 * WAVES)
                 if (idx & 16) st128(lds0 + S::C_OFF + idx * 16, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
         }
         __syncthreads();
@@ -347,12 +356,12 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     auto step = [&](auto exp_tag, auto qk_tag, auto pv_tag, auto stage_tag, u32x4 (&pf_in)[2], u32x4 (&pf_out)[2], int key0, int e0, int e1, int qk_tile,
                     int qk_kb, int pv_tile, int pv_kb, int next_tile, int next_kb, Staging &g, int st_tile) __attribute__((always_inline)) {
         constexpr bool EXP = decltype(exp_tag)::value, QK = decltype(qk_tag)::value, PV = decltype(pv_tag)::value;
-        constexpr int STAGE = decltype(stage_tag)::value;  // 0: none, 1: first half of the parts, 2: second half
+        constexpr int STAGE = decltype(stage_tag)::value;  // 0: none, 1: first half of the parts, 2: second half, 3: all
         const uint32_t ka = lds0 + (qk_tile & 1) * 16384 + qk_kb * 8192 + lane * 16;
-        const uint32_t va = lds0 + S::V_OFF + (pv_tile % 3) * 16384 + pv_kb * 8192 + lane * 16;
-        const uint32_t ca = lds0 + S::C_OFF + (pv_tile % 3) * S::C_TILE + pv_kb * 2 * NRB * 1024 + lane * 16;
-        const uint32_t vn = lds0 + S::V_OFF + (next_tile % 3) * 16384 + next_kb * 8192 + lane * 16;
-        const uint32_t cn = lds0 + S::C_OFF + (next_tile % 3) * S::C_TILE + next_kb * 2 * NRB * 1024 + lane * 16;
+        const uint32_t va = lds0 + S::V_OFF + (pv_tile % VT) * 16384 + pv_kb * 8192 + lane * 16;
+        const uint32_t ca = lds0 + S::C_OFF + (pv_tile % VT) * S::C_TILE + pv_kb * 2 * NRB * 1024 + lane * 16;
+        const uint32_t vn = lds0 + S::V_OFF + (next_tile % VT) * 16384 + next_kb * 8192 + lane * 16;
+        const uint32_t cn = lds0 + S::C_OFF + (next_tile % VT) * S::C_TILE + next_kb * 2 * NRB * 1024 + lane * 16;
         // operands in order: those of the values (page i / (4 + NRB), block i % (4 + NRB)), of the scores, then the next step's first
         auto frag = [&](auto slot_tag) __attribute__((always_inline)) -> u32x4 {
             constexpr int slot = decltype(slot_tag)::value;
@@ -435,7 +444,10 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
                     if constexpr (!LROW) lsum += tsum;
                 }
             }
-            if constexpr (STAGE > 0 && i >= NP) {
+            if constexpr (STAGE == 3) {
+                constexpr int p0 = PARTS * i / SLOTS, p1 = PARTS * (i + 1) / SLOTS;
+                each<p1 - p0>([&](auto k) __attribute__((always_inline)) { stage_part(g, st_tile, std::integral_constant<int, p0 + k.value>{}); });
+            } else if constexpr (STAGE > 0 && i >= NP) {
                 constexpr int HALF = PARTS / 2, q = i - NP, p0 = HALF * q / 8, p1 = HALF * (q + 1) / 8;
                 each<p1 - p0>([&](auto k) __attribute__((always_inline)) {
                     stage_part(g, st_tile, std::integral_constant<int, (STAGE - 1) * HALF + p0 + k.value>{});
@@ -459,30 +471,84 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     using N0 = std::integral_constant<int, 0>;
     using N1 = std::integral_constant<int, 1>;
     using N2 = std::integral_constant<int, 2>;
+    using N3 = std::integral_constant<int, 3>;
     Staging g;
-    u32x4 pa[2], pb[2];  // weights of a tile's second and first half [page]
+    u32x4 pa[2], pb[2];  // weights [page]: of a tile's second and first half; two key groups: of the tile before and of a tile
 
     request_angles(0, 0);
     each<PARTS>([&](auto i) __attribute__((always_inline)) { stage_part(g, 0, i); });  // (requests tile 1)
     __syncthreads();
-    // tile 0: no values yet
     auto exps_of = [&](int tile) __attribute__((always_inline)) { return *reinterpret_cast<const i32x4 *>(page_exp + (tile & 1) * 4); };
-    i32x4 e = exps_of(0);
-    request_angles(1, 0);
-    step(F{}, T{}, F{}, N1{}, pa, pb, 0, 0, 0, 0, 0, 0, 0, 0, 0, g, 1);
-    step(T{}, T{}, F{}, N2{}, pa, pb, 0, e.x, e.y, 0, 1, 0, 0, 0, 0, g, 1);
-    for (int u = 1; u < n_tiles; ++u) {
-        lds_fence_barrier();  // (not one that waits for the loads in flight) tile u is staged, tile u - 1's keys and tile u - 2's values are read
-        const i32x4 en = exps_of(u);
-        request_angles(u + 1, 0);
-        step(T{}, T{}, T{}, N1{}, pb, pa, (u - 1) * TILE_KEYS + 32, e.z, e.w, u, 0, u - 1, 0, u - 1, 1, g, u + 1);
-        step(T{}, T{}, T{}, N2{}, pa, pb, u * TILE_KEYS, en.x, en.y, u, 1, u - 1, 1, u, 0, g, u + 1);
-        e = en;
+    if constexpr (KG == 1) {
+        // tile 0: no values yet
+        i32x4 e = exps_of(0);
+        request_angles(1, 0);
+        step(F{}, T{}, F{}, N1{}, pa, pb, 0, 0, 0, 0, 0, 0, 0, 0, 0, g, 1);
+        step(T{}, T{}, F{}, N2{}, pa, pb, 0, e.x, e.y, 0, 1, 0, 0, 0, 0, g, 1);
+        for (int u = 1; u < n_tiles; ++u) {
+            lds_fence_barrier();  // (not one that waits for the loads in flight) tile u is staged, tile u - 1's keys and tile u - 2's values are read
+            const i32x4 en = exps_of(u);
+            request_angles(u + 1, 0);
+            step(T{}, T{}, T{}, N1{}, pb, pa, (u - 1) * TILE_KEYS + 32, e.z, e.w, u, 0, u - 1, 0, u - 1, 1, g, u + 1);
+            step(T{}, T{}, T{}, N2{}, pa, pb, u * TILE_KEYS, en.x, en.y, u, 1, u - 1, 1, u, 0, g, u + 1);
+            e = en;
+        }
+        // the last tile's second half, and its values
+        step(T{}, F{}, T{}, N0{}, pb, pa, (n_tiles - 1) * TILE_KEYS + 32, e.z, e.w, 0, 0, n_tiles - 1, 0, n_tiles - 1, 1, g, 0);
+        step(F{}, F{}, T{}, N0{}, pa, pb, 0, 0, 0, 0, 0, n_tiles - 1, 1, 0, 0, g, 0);
+    } else {
+        // Key group kg takes half kg of every tile, one step per tile: values of tile u - 2, weights of u - 1, scores of u.  (Before there
+        // are weights, tile 0's values meet zeros.)
+        auto pages_of = [&](int tile) __attribute__((always_inline)) { return *reinterpret_cast<const u32x2 *>(page_exp + (tile & 1) * 4 + 2 * kg); };
+        u32x2 e = pages_of(0);
+        pa[0] = pa[1] = u32x4{0, 0, 0, 0};
+        request_angles(1, 0);
+        step(F{}, T{}, F{}, N3{}, pa, pb, 0, 0, 0, 0, kg, 0, 0, 0, kg, g, 1);
+        for (int u = 1; u < n_tiles; ++u) {
+            lds_fence_barrier();  // tile u is staged, tile u - 1's keys and tile u - 3's values are read
+            const u32x2 en = pages_of(u);
+            request_angles(u + 1, 0);
+            step(T{}, T{}, T{}, N3{}, pa, pb, (u - 1) * TILE_KEYS + 32 * kg, e.x, e.y, u, kg, max(u - 2, 0), kg, u - 1, kg, g, u + 1);
+            pa[0] = pb[0];
+            pa[1] = pb[1];
+            e = en;
+        }
+        step(T{}, F{}, T{}, N0{}, pa, pb, (n_tiles - 1) * TILE_KEYS + 32 * kg, e.x, e.y, 0, 0, max(n_tiles - 2, 0), kg, n_tiles - 1, kg, g, 0);
+        step(F{}, F{}, T{}, N0{}, pb, pa, 0, 0, 0, 0, 0, n_tiles - 1, kg, 0, 0, g, 0);
     }
-    // the last tile's second half, and its values
-    step(T{}, F{}, T{}, N0{}, pb, pa, (n_tiles - 1) * TILE_KEYS + 32, e.z, e.w, 0, 0, n_tiles - 1, 0, n_tiles - 1, 1, g, 0);
-    step(F{}, F{}, T{}, N0{}, pa, pb, 0, 0, 0, 0, 0, n_tiles - 1, 1, 0, 0, g, 0);
     __syncthreads();
+    if constexpr (KG == 2) {  // the second key group leaves its rows in LDS, the first merges them into its own
+        constexpr int NF4 = S::NF4;
+        f32x4 *buf = reinterpret_cast<f32x4 *>(lds) + rg * NF4 * 64 + lane;
+        auto four = [](const f32x16 &x, int i) __attribute__((always_inline)) { return f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]}; };
+        if (kg == 1) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) buf[i * 64] = four(oacc[i / 4], i % 4);
+#pragma unroll
+            for (int i = 0; i < 4 * NRB; ++i) buf[(16 + i) * 64] = four(racc[i / 4], i % 4);
+            buf[(NF4 - 1) * 64] = f32x4{m_run, lsum, 0.f, 0.f};
+        }
+        __syncthreads();
+        if (kg == 0) {
+            const f32x4 ml = buf[(NF4 - 1) * 64];
+            const float M = fmaxf(m_run, ml.x), Mu = M == kNegInf ? 0.f : M;
+            const float w0 = fast_exp2(m_run - Mu), w1 = fast_exp2(ml.x - Mu);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const f32x4 x = buf[i * 64];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) oacc[i / 4][4 * (i % 4) + j] = oacc[i / 4][4 * (i % 4) + j] * w0 + x[j] * w1;
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * NRB; ++i) {
+                const f32x4 x = buf[(16 + i) * 64];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) racc[i / 4][4 * (i % 4) + j] = racc[i / 4][4 * (i % 4) + j] * w0 + x[j] * w1;
+            }
+            lsum = lsum * w0 + ml.y * w1;
+        }
+        __syncthreads();
+    }
 
     // ---- epilogue: O = (acc + acc_r . B_V[h]) / l; lane: row r32, dims 32 b + 8 (i / 4) + 4 hh + i % 4 ----
     const float l_run = LROW ? __shfl(racc[0][8], r32) : lsum + __shfl_xor(lsum, 32);
@@ -499,12 +565,13 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int rho = 32 * b + 8 * (i / 4) + 4 * hh + i % 4;
-                if (rho < R) acc[(wave * 32 + r32) * (R + 1) + rho] = racc[b][i];
+                if (rho < R && kg == 0) acc[(rg * 32 + r32) * (R + 1) + rho] = racc[b][i];
             }
         __syncthreads();
+        if (kg > 0) return;
 #pragma unroll 2
         for (int rho = 0; rho < R; ++rho) {
-            const float x = acc[(wave * 32 + r32) * (R + 1) + rho];
+            const float x = acc[(rg * 32 + r32) * (R + 1) + rho];
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -515,9 +582,9 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
                 }
         }
     }
-    if (row_tok >= 0) {
+    if (kg == 0 && row_tok >= 0) {
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-        uint16_t *o = p.out + ((int64_t)(q0 + row_tok) * p.hq + h * G + (wave * 32 + r32) % G) * D;
+        uint16_t *o = p.out + ((int64_t)(q0 + row_tok) * p.hq + h * G + (rg * 32 + r32) % G) * D;
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -528,10 +595,10 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     }
 }
 
-template <int R, int G, bool ROPE>
+template <int R, int G, bool ROPE, int KG>
 __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_stream_kernel(PrefillArgs p) {
-    constexpr int TPW = ROWS / G;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[Lay<R>::BYTES > Lay<0>::BYTES ? Lay<R>::BYTES : Lay<0>::BYTES];
+    constexpr int TPW = Lay<R, KG>::ROWS / G;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[Lay<R, KG>::BYTES > Lay<0, KG>::BYTES ? Lay<R, KG>::BYTES : Lay<0, KG>::BYTES];
     const int bpa = p.blocks_per_agent_head;
     const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
     const int pair = (local / bpa) * kXcds + xcd, qb = local % bpa;
@@ -541,36 +608,42 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_stream_kernel(Prefi
     const int tok_begin = qb * TPW;
     if (qb == bpa - 1 && nq > bpa * TPW) poison_unreached_rows(p, q0, nq, h, G, bpa * TPW);
     if (tok_begin >= nq) return;
-    if (R > 0 && p.adapter_idx[a] >= 0) block<R, G, ROPE>(p, lds, a, h, tok_begin);
-    else block<0, G, false>(p, lds, a, h, tok_begin);
+    if (R > 0 && p.adapter_idx[a] >= 0) block<R, G, ROPE, KG>(p, lds, a, h, tok_begin);
+    else block<0, G, false, KG>(p, lds, a, h, tok_begin);
 }
 
-template <int R, int G, bool ROPE>
+template <int R, int G, bool ROPE, int KG>
 hipError_t launch(const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     const int pairs = (pa.n_agents * pa.hkv + kXcds - 1) / kXcds * kXcds;
     // timing events carry the kernel's own start and end timestamps (set by the launch)
     hipEvent_t e0 = ev ? static_cast<hipEvent_t>(ev[0]) : nullptr, e1 = ev ? static_cast<hipEvent_t>(ev[1]) : nullptr;
-    hipExtLaunchKernelGGL((prefill_fp8_stream_kernel<R, G, ROPE>), dim3(pairs * pa.blocks_per_agent_head), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
+    hipExtLaunchKernelGGL((prefill_fp8_stream_kernel<R, G, ROPE, KG>), dim3(pairs * pa.blocks_per_agent_head), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
     return hipGetLastError();
 }
 
-template <int G>
+template <int R, int G, int KG>
+hipError_t launch(bool rope, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+    return R > 0 && rope ? launch<R, G, (R > 0), KG>(pa, st, ev) : launch<R, G, false, KG>(pa, st, ev);
+}
+
+template <int G, int KG>
 hipError_t dispatch(int r, bool rope, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     switch (r) {
-    case 0: return launch<0, G, false>(pa, st, ev);
-    case 8: return rope ? launch<8, G, true>(pa, st, ev) : launch<8, G, false>(pa, st, ev);
-    case 16: return rope ? launch<16, G, true>(pa, st, ev) : launch<16, G, false>(pa, st, ev);
-    case 32: return rope ? launch<32, G, true>(pa, st, ev) : launch<32, G, false>(pa, st, ev);
-    case 64: return rope ? launch<64, G, true>(pa, st, ev) : launch<64, G, false>(pa, st, ev);
+    case 0: return launch<0, G, KG>(rope, pa, st, ev);
+    case 8: return launch<8, G, KG>(rope, pa, st, ev);
+    case 16: return launch<16, G, KG>(rope, pa, st, ev);
+    case 32: return launch<32, G, KG>(rope, pa, st, ev);
+    case 64: return launch<64, G, KG>(rope, pa, st, ev);
     default: return hipErrorInvalidValue;
     }
 }
 
 }  // namespace
 
-hipError_t launch_fp8_stream(int r, int g, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
-    const bool rope = r > 0 && pa.rope_cos;
-    return g == 4 ? dispatch<4>(r, rope, pa, st, ev) : dispatch<8>(r, rope, pa, st, ev);
+hipError_t launch_fp8_stream(int r, int g, int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+    const bool rope = pa.rope_cos != nullptr;
+    if (rows == 256) return g == 4 ? dispatch<4, 1>(r, rope, pa, st, ev) : dispatch<8, 1>(r, rope, pa, st, ev);
+    return g == 4 ? dispatch<4, 2>(r, rope, pa, st, ev) : dispatch<8, 2>(r, rope, pa, st, ev);
 }
 
 }  // namespace fkvp

@@ -248,6 +248,13 @@ def test_prefill_tiles(r, rope, lens, rows):
     p.check(p.prefill())
 
 
+@pytest.mark.parametrize("r,rope", RANKS)
+def test_prefill_middle_grids(r, rope):
+    """Grids that fill the compute units with 128 rows per workgroup and not with 256: contexts of one tile to many, whole and partial."""
+    p = Problem(14, [1000, 63, 250, 4130], 0, 32, 8, r, rope, rows=[250, 63, 250, 249], bare=(0,))
+    p.check(p.prefill())
+
+
 @pytest.mark.parametrize("r", [0, 16])
 def test_prefill_understated_rows_are_nan(r):
     p = Problem(13, [400, 300], 0, 32, 8, r, False, rows=[200, 20])
