@@ -145,6 +145,7 @@ fkv_residual_attention_decode_fp8 = _sig("fkv_residual_attention_decode_fp8", c_
                                          [ctypes.POINTER(fkv_attn_args), c_vp, c_vp])
 fkv_residual_attention_prefill_fp8 = _sig("fkv_residual_attention_prefill_fp8", c_i32,
                                           [ctypes.POINTER(fkv_attn_args), c_vp])
+fkv_prefill_fp8_workspace_bytes = _sig("fkv_prefill_fp8_workspace_bytes", c_i64, [c_i32] * 6)
 
 
 class fkv_read_seq(ctypes.Structure):

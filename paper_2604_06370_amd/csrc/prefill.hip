@@ -657,7 +657,7 @@ fkv_status prefill_impl(const fkv_attn_args *a, void *stream, bool fp8) {
     hipStream_t hs = static_cast<hipStream_t>(stream);
     hipError_t e;
     if (fp8) {
-        e = launch_fp8(a->r, g, maxq, pa, hs, a->timing_events);
+        e = launch_fp8(a->r, g, maxq, pa, a->workspace, a->workspace_bytes, hs, a->timing_events);
     } else {
         const PrefillForm form = prefill_form(a->r, rope, g, (int64_t)a->n_agents * a->hkv, maxq);
         pa.blocks_per_agent_head = (int)(((int64_t)maxq * g + 255) / 256) * (256 / form.rows);
@@ -681,6 +681,8 @@ extern "C" fkv_status fkv_residual_attention_prefill_fp8(const fkv_attn_args *a,
     fkv::clear_error();
     if (a && ((uintptr_t)a->base_kv & 15))
         return fkv::fail(FKV_ERR_INVALID, "fkv_residual_attention_prefill_fp8: the base pool must be aligned to 16 bytes");
+    if (a && ((uintptr_t)a->workspace & 15))
+        return fkv::fail(FKV_ERR_INVALID, "fkv_residual_attention_prefill_fp8: the workspace must be aligned to 16 bytes");
     return prefill_impl(a, stream, true);
 }
 

@@ -15,6 +15,10 @@ struct PrefillArgs {
     int32_t n_agents, hq, hkv, max_pages, blocks_per_agent_head;
     float scale_log2;
     int32_t rope_rows;  // positions the RoPE tables hold
+    // 8-bit pages: each agent's keys are split over `splits` workgroups, which leave partial rows in `parts`, records of `part_stride`
+    // floats [split][agent][token of the chunk, of `reach`][query head]: acc[128], acc_r[R], m and l at part_stride - 4
+    float *parts;
+    int32_t splits, reach, part_stride;
 };
 
 constexpr int kXcds = 8;
@@ -37,8 +41,19 @@ __device__ __forceinline__ void poison_unreached_rows(const PrefillArgs &p, int 
 // Launch of the pipelined kernel (prefill_stream.hip) with 128 or 256 query rows per workgroup.
 hipError_t launch_stream(int r, int g, bool rope, bool rows128, const PrefillArgs &pa, hipStream_t st, void *const *ev);
 
-// Launch of the kernels over 8-bit base pages (prefill_fp8.hip), which sets blocks_per_agent_head for chunks of up to max_q tokens.
-hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev);
+__device__ __forceinline__ float *partial_row(const PrefillArgs &p, int split, int a, int tok, int head) {
+    return p.parts + ((((int64_t)split * p.n_agents + a) * p.reach + tok) * p.hq + head) * p.part_stride;
+}
+// A workgroup without keys in its split leaves rows of no weight.
+__device__ __forceinline__ void empty_rows(const PrefillArgs &p, int split, int a, int h, int g, int tok_begin, int tok_end) {
+    for (int i = threadIdx.x; i < (tok_end - tok_begin) * g; i += blockDim.x)
+        *reinterpret_cast<fkvk::f32x4 *>(partial_row(p, split, a, tok_begin + i / g, h * g + i % g) + p.part_stride - 4) =
+            fkvk::f32x4{-INFINITY, 0.f, 0.f, 0.f};
+}
+
+// Launch of the kernels over 8-bit base pages (prefill_fp8.hip) for chunks of up to max_q tokens, which sets the fields of the grid. Keys are
+// split only where `workspace` has the bytes for it.
+hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, void *workspace, size_t workspace_bytes, hipStream_t st, void *const *ev);
 
 // The one of all but small grids (prefill_fp8_stream.hip): 256 or 128 query rows per workgroup.
 hipError_t launch_fp8_stream(int r, int g, int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev);

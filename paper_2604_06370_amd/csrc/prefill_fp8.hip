@@ -1,14 +1,15 @@
 // ResidualAttention chunked prefill over 8-bit base pages (Section 6 prefill kernel, Algorithm 1 with a block of
 // query rows; fp8_cache.hpp has the page format).
 //
-// One workgroup of eight waves = (agent a, KV head h, block of 32 NRG query rows); its rows are (query token, query head of
-// h), all of the same agent.  Wave w serves row group w % NRG (32 rows) as key group w / NRG.  Per round of eight pages:
+// The kernel of small grids: one workgroup of eight waves = (agent a, KV head h, block of 64 query rows, split of the keys); its rows are
+// (query token, query head of h), all of the same agent.  Wave w serves row group w % 2 (32 rows) as key group w / 2.  Per round of
+// eight pages:
 //   staging     wave w takes page w: its codes and rCache rows come to registers one round ahead, and leave as
 //               matrix-core operands in LDS, where all waves read them: a value is converted once per workgroup.
 //               K = K_base + RoPE_p(B_K^T C_K^T) (without tables no rotation), V = code * 2^E.
-//   every wave  S^T = K Q^T, causal mask + online softmax, O^T += V^T P^T, acc_r^T += C_V^T P^T over its 8 NRG / 8 pages
-// and at the end the key groups' rows are merged and O = (O + acc_r . B_V[h]) / l (Eq. 4) is written in bf16.  This is the kernel of
-// workgroups of 64 and 32 rows, where more would leave compute units idle; prefill_fp8_stream.hip has the one of 256 and 128.
+//   every wave  S^T = K Q^T, causal mask + online softmax, O^T += V^T P^T, acc_r^T += C_V^T P^T over the two pages of its key group
+// and at the end the key groups' rows are merged and O = (O + acc_r . B_V[h]) / l (Eq. 4) is written in bf16, or, where the keys are
+// split over workgroups, the partial rows for merge_splits_kernel.  prefill_fp8_stream.hip has the kernel of 256 and 128 rows.
 //
 // K and Q are fp16 here, 11 significant bits: the sum of a base key, exact in four bits, and its low-rank part would
 // lose what bf16 keeps of it alone (error of the result 5.6e-3 with bf16 keys at 8B heads, rank 16, over 9000 tokens, 2-norm; 2.2e-3 in
@@ -18,6 +19,7 @@
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "fp8_cache.hpp"
@@ -32,18 +34,18 @@ namespace {
 
 constexpr int D = 128, PS = 16;
 constexpr int WAVES = 8, ROWS_PER_WAVE = 32, ROUND_PAGES = WAVES, ROUND_KEYS = ROUND_PAGES * PS;
+constexpr int NRG = 2, KG = WAVES / NRG, ROWS = NRG * ROWS_PER_WAVE, GP = ROUND_PAGES / KG;  // row groups, key groups; pages of a key group per round
 constexpr float kNegInf = -INFINITY, kLazyRescale = 8.f;
 
-template <int R, int NRG>
+template <int R>
 struct Shape {
     static constexpr int RT = R == 0 ? 0 : (R + 15) / 16, RTX = RT > 0 ? RT : 1;
-    static constexpr int ROWS = NRG * ROWS_PER_WAVE, KG = WAVES / NRG, GP = ROUND_PAGES / KG;  // pages of a key group per round
     // LDS: K and V ([page][4 KB], fragment order), rCache pages [page][rank tile][1 KB], B_K^T fragments, page exponents
     static constexpr int V_OFF = ROUND_PAGES * 4096, C_OFF = 2 * V_OFF, B_OFF = C_OFF + RT * ROUND_PAGES * 1024;
     static constexpr int E_OFF = B_OFF + RT * 4096, MAIN = E_OFF + 64;
     static constexpr int EPI = R * D * 4 + ROWS * (R + 1) * 4;  // B_V and the rank accumulators of the epilogue
     static constexpr int NF4 = 2 * (8 + RT + 2);                // a wave's rows: oacc, racc, lacc, m
-    static constexpr int MERGE = KG > 1 ? (KG / 2) * NRG * NF4 * 1024 : 0;
+    static constexpr int MERGE = (KG / 2) * NRG * NF4 * 1024;
     static constexpr int B2 = MAIN > EPI ? MAIN : EPI;
     static constexpr int BYTES = B2 > MERGE ? B2 : MERGE;
     static_assert(BYTES <= 160 * 1024, "LDS of one workgroup");
@@ -55,19 +57,19 @@ __device__ __forceinline__ u32x2 value_word(uint32_t w, const f32x4 &scale) {
     return u32x2{pack_bf16(lo.x * scale.x, lo.y * scale.y), pack_bf16(hi.x * scale.z, hi.y * scale.w)};
 }
 
-template <int R, int G, int NRG>
+template <int R, int G>
 __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs p) {
-    using S = Shape<R, NRG>;
-    constexpr int RT = S::RT, RTX = S::RTX, TPW = S::ROWS / G, GP = S::GP;
+    using S = Shape<R>;
+    constexpr int RT = S::RT, RTX = S::RTX, TPW = ROWS / G;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[S::BYTES];
     const int hkv = p.hkv, bpa = p.blocks_per_agent_head;
     const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
-    const int pair = (local / bpa) * kXcds + xcd, qb = local % bpa;
+    const int pair = local / (bpa * p.splits) * kXcds + xcd, qb = local % bpa, split = local / bpa % p.splits;
     if (pair >= p.n_agents * hkv) return;
     const int a = pair / hkv, h = pair % hkv;
     const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
     const int tok_begin = qb * TPW;
-    if (qb == bpa - 1 && nq > bpa * TPW) poison_unreached_rows(p, q0, nq, h, G, bpa * TPW);
+    if (qb == bpa - 1 && split == 0 && nq > bpa * TPW) poison_unreached_rows(p, q0, nq, h, G, bpa * TPW);
     if (tok_begin >= nq) return;
     const int L = p.seq_lens[a], P0 = L - nq;
     const int ad = R > 0 ? p.adapter_idx[a] : -1;
@@ -78,8 +80,11 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     const int rg = wave % NRG, kg = wave / NRG;
     const int64_t n = (int64_t)hkv * D;
     const int n_pages = (L + PS - 1) / PS;
-    const int last_pos = P0 + (tok_begin + TPW < nq ? tok_begin + TPW : nq) - 1;
-    const int n_rounds = last_pos / ROUND_KEYS + 1;
+    const int tok_end = tok_begin + TPW < nq ? tok_begin + TPW : nq, last_pos = P0 + tok_end - 1;
+    // rounds of this split: n_rounds from r0 (rounds below are counted from r0)
+    const int all_rounds = last_pos / ROUND_KEYS + 1, per_split = (all_rounds + p.splits - 1) / p.splits, r0 = split * per_split;
+    const int n_rounds = min(per_split, all_rounds - r0);
+    if (n_rounds <= 0) return empty_rows(p, split, a, h, G, tok_begin, tok_end);
     const int32_t *btb = p.base_bt + (int64_t)a * p.max_pages, *btr = R > 0 ? p.res_bt + (int64_t)a * p.max_pages : nullptr;
     const unsigned char *base = reinterpret_cast<const unsigned char *>(p.base_kv);
 
@@ -90,7 +95,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     f32x4 cs[4], sn[4];
     // Page ids of this wave's pages of 64 rounds, one per lane, and of the 64 after them: an id read where it is used would hold up the wave.
     auto ids = [&](int chunk, int &b, int &r) __attribute__((always_inline)) {
-        const int pg = min((64 * chunk + lane) * ROUND_PAGES + wave, n_pages - 1);  // pages past the sequence repeat its last one; their keys are masked
+        const int pg = min((r0 + 64 * chunk + lane) * ROUND_PAGES + wave, n_pages - 1);  // pages past the sequence repeat its last one; their keys are masked
         b = btb[pg];
         r = R > 0 ? btr[pg] : 0;
     };
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
             idr = idr_next;
             ids((round >> 6) + 1, idb_next, idr_next);
         }
-        const int pg = min(ROUND_PAGES * round + wave, n_pages - 1);
+        const int pg = min(ROUND_PAGES * (r0 + round) + wave, n_pages - 1);
         const unsigned char *page = base + (int64_t)__builtin_amdgcn_readlane(idb, round & 63) * f8_page_bytes(hkv);
         const unsigned char *blk = page + (int64_t)h * kF8HeadBytes + lane * 16;
         const unsigned char *ex = page + f8_exp_off(hkv, h);
@@ -134,7 +139,7 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     int *page_exp = reinterpret_cast<int *>(lds + S::E_OFF);
     float b_sum = 0.f;  // sum over ranks of sqrt(2) max_i |B_K[rho][i]|
     auto stage = [&](int round) __attribute__((always_inline)) {
-        const int vis = L - (ROUND_PAGES * round + wave) * PS;  // tokens of the page inside the sequence
+        const int vis = L - (ROUND_PAGES * (r0 + round) + wave) * PS;  // tokens of the page inside the sequence
         if (vis < PS) {  // unwritten values may be any bits, and meet zero weights
             const int left = max(0, min(4, vis - 4 * grp));
             const uint32_t m = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
@@ -302,14 +307,13 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     float m_run[2] = {kNegInf, kNegInf};
     const float cl = p.scale_log2;
     const u32x4 kOnes = u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
-    constexpr int CP = GP < 4 ? GP : 4;  // pages of one softmax step
 
-    // Pages pg0 .. pg0 + CP - 1 of the round in LDS, keys from key0.
+    // Pages pg0 .. pg0 + GP - 1 of the round in LDS, keys from key0.
     auto step = [&](int pg0, int key0) __attribute__((always_inline)) {
-        f32x4 sacc[CP][2];
-        int ep[CP];
+        f32x4 sacc[GP][2];
+        int ep[GP];
 #pragma unroll
-        for (int kt = 0; kt < CP; ++kt) {
+        for (int kt = 0; kt < GP; ++kt) {
             ep[kt] = page_exp[pg0 + kt];
             sacc[kt][0] = sacc[kt][1] = f32x4{0, 0, 0, 0};
 #pragma unroll
@@ -321,20 +325,20 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
         }
         // causal mask and online softmax (rows in lanes): the maximum moves, and the accumulators are rescaled, only
         // where a row's scores exceed it by more than 2^kLazyRescale
-        const bool full = key0 + CP * PS - 1 <= P0 + tok_begin;
-        u32x2 pf[CP][2];
+        const bool full = key0 + GP * PS - 1 <= P0 + tok_begin;
+        u32x2 pf[GP][2];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
             if (!full) {
                 const int lim = row_tok[nt] < 0 ? -1 : P0 + row_tok[nt] - key0 - 4 * grp;
 #pragma unroll
-                for (int kt = 0; kt < CP; ++kt)
+                for (int kt = 0; kt < GP; ++kt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sacc[kt][nt][i] = kt * PS + i <= lim ? sacc[kt][nt][i] : kNegInf;
             }
-            float mx = kNegInf, f[CP];
+            float mx = kNegInf, f[GP];
 #pragma unroll
-            for (int kt = 0; kt < CP; ++kt) {
+            for (int kt = 0; kt < GP; ++kt) {
                 f[kt] = fminf(fmaxf(ldexpf(cl, ep[kt] + eq[nt]), 1.2e-38f), 3e38f);  // neither 0 nor infinite: masked scores and zeros stay
                 float x = sacc[kt][nt][0];
 #pragma unroll
@@ -354,47 +358,39 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
             }
             const float m_use = m_run[nt] == kNegInf ? 0.f : m_run[nt];
 #pragma unroll
-            for (int kt = 0; kt < CP; ++kt) {
+            for (int kt = 0; kt < GP; ++kt) {
                 f32x4 pv;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pv[i] = fast_exp2(__builtin_fmaf(sacc[kt][nt][i], f[kt], -m_use));
                 pf[kt][nt] = pack4(pv);
             }
         }
-        // values, two pages (32 keys) per product (one page: its upper half is zero); row sums of the weights as the products take them
-        constexpr bool TWO = CP > 1;
+        // values, two pages (32 keys) per product; row sums of the weights as the products take them
+        u32x4 pb[2];
 #pragma unroll
-        for (int hf = 0; hf < (TWO ? CP / 2 : 1); ++hf) {
-            u32x4 pb[2];
+        for (int nt = 0; nt < 2; ++nt) pb[nt] = u32x4{pf[0][nt].x, pf[0][nt].y, pf[1][nt].x, pf[1][nt].y};
+        const unsigned char *vb = lds + S::V_OFF + pg0 * 4096 + lane * 16;
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt)
-                pb[nt] = u32x4{pf[TWO ? 2 * hf : 0][nt].x, pf[TWO ? 2 * hf : 0][nt].y, TWO ? pf[TWO ? 2 * hf + 1 : 0][nt].x : 0u,
-                               TWO ? pf[TWO ? 2 * hf + 1 : 0][nt].y : 0u};
-            const unsigned char *vb = lds + S::V_OFF + (pg0 + 2 * hf) * 4096 + lane * 16;
+        for (int q2 = 0; q2 < 4; ++q2) {
+            const u32x4 v0 = *reinterpret_cast<const u32x4 *>(vb + q2 * 1024), v1 = *reinterpret_cast<const u32x4 *>(vb + 4096 + q2 * 1024);
+            const u32x4 va = {v0.x, v0.y, v1.x, v1.y}, vc = {v0.z, v0.w, v1.z, v1.w};  // dims 32 q2 + col, 32 q2 + 16 + col
 #pragma unroll
-            for (int q2 = 0; q2 < 4; ++q2) {
-                const u32x4 v0 = *reinterpret_cast<const u32x4 *>(vb + q2 * 1024);
-                const u32x4 v1 = TWO ? *reinterpret_cast<const u32x4 *>(vb + 4096 + q2 * 1024) : u32x4{0, 0, 0, 0};
-                const u32x4 va = {v0.x, v0.y, v1.x, v1.y}, vc = {v0.z, v0.w, v1.z, v1.w};  // dims 32 q2 + col, 32 q2 + 16 + col
-#pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    oacc[2 * q2][nt] = mfma32(va, pb[nt], oacc[2 * q2][nt]);
-                    oacc[2 * q2 + 1][nt] = mfma32(vc, pb[nt], oacc[2 * q2 + 1][nt]);
-                }
+            for (int nt = 0; nt < 2; ++nt) {
+                oacc[2 * q2][nt] = mfma32(va, pb[nt], oacc[2 * q2][nt]);
+                oacc[2 * q2 + 1][nt] = mfma32(vc, pb[nt], oacc[2 * q2 + 1][nt]);
             }
+        }
 #pragma unroll
-            for (int nt = 0; nt < 2; ++nt) lacc[nt] = mfma32(kOnes, pb[nt], lacc[nt]);
-            if constexpr (R > 0) {
-                if (use_res) {
+        for (int nt = 0; nt < 2; ++nt) lacc[nt] = mfma32(kOnes, pb[nt], lacc[nt]);
+        if constexpr (R > 0) {
+            if (use_res) {
 #pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        const unsigned char *cb = lds + S::C_OFF + ((pg0 + 2 * hf) * RT + t) * 1024 + lane * 16 + 8;
-                        const u32x2 c0 = *reinterpret_cast<const u32x2 *>(cb);
-                        const u32x2 c1 = TWO ? *reinterpret_cast<const u32x2 *>(cb + RT * 1024) : u32x2{0, 0};
-                        const u32x4 ca = {c0.x, c0.y, c1.x, c1.y};
+                for (int t = 0; t < RT; ++t) {
+                    const unsigned char *cb = lds + S::C_OFF + (pg0 * RT + t) * 1024 + lane * 16 + 8;
+                    const u32x2 c0 = *reinterpret_cast<const u32x2 *>(cb), c1 = *reinterpret_cast<const u32x2 *>(cb + RT * 1024);
+                    const u32x4 ca = {c0.x, c0.y, c1.x, c1.y};
 #pragma unroll
-                        for (int nt = 0; nt < 2; ++nt) racc[t][nt] = mfma32(ca, pb[nt], racc[t][nt]);
-                    }
+                    for (int nt = 0; nt < 2; ++nt) racc[t][nt] = mfma32(ca, pb[nt], racc[t][nt]);
                 }
             }
         }
@@ -406,17 +402,14 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
         stage(round);
         if (round + 1 < n_rounds) request(round + 1);
         lds_fence_barrier();  // (not one that waits for the loads in flight)
-#pragma unroll
-        for (int s = 0; s < GP; s += CP) {
-            const int key0 = round * ROUND_KEYS + (kg * GP + s) * PS;
-            if (key0 <= last_pos) step(kg * GP + s, key0);
-        }
+        const int key0 = (r0 + round) * ROUND_KEYS + kg * GP * PS;
+        if (key0 <= last_pos) step(kg * GP, key0);
     }
     __syncthreads();
 
     // ---- key groups: the upper half leaves its rows in LDS, the lower half merges them into its own ----
 #pragma unroll
-    for (int half = S::KG / 2; half > 0; half /= 2) {
+    for (int half = KG / 2; half > 0; half /= 2) {
         f32x4 *buf = reinterpret_cast<f32x4 *>(lds) + lane;
         if (kg >= half && kg < 2 * half) {
             f32x4 *dst = buf + ((kg - half) * NRG + rg) * S::NF4 * 64;
@@ -448,6 +441,21 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
         __syncthreads();
     }
 
+    if (p.splits > 1) {  // this split's partial rows
+        if (kg > 0) return;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            if (row_tok[nt] < 0) continue;
+            float *rec = partial_row(p, split, a, row_tok[nt], h * G + (rg * ROWS_PER_WAVE + nt * 16 + col) % G);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) *reinterpret_cast<f32x4 *>(rec + 16 * m + 4 * grp) = oacc[m][nt];
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+                if (16 * t + 4 * grp < R) *reinterpret_cast<f32x4 *>(rec + D + 16 * t + 4 * grp) = racc[t][nt];
+            if (grp == 0) *reinterpret_cast<f32x4 *>(rec + p.part_stride - 4) = f32x4{m_run[nt], lacc[nt][0], 0.f, 0.f};
+        }
+        return;
+    }
     // ---- epilogue: O = (acc + acc_r . B_V[h]) / l ----
     if constexpr (R > 0) {
         if (use_res) {
@@ -487,52 +495,142 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     }
 }
 
-// Rows per workgroup: the most (of 256, 128, 64, 32) whose workgroups still fill every compute unit of the fullest XCD (an (agent,
-// KV head) pair keeps to one XCD), else 32.  Four chunks of up to 250 tokens over 35k, 8B heads: 128 rows 939 us, 256 rows 1214 us;
-// eight of up to 1024 over 9.5k, RoPE: 256 rows 1664 us, 128 rows 2168 us (this file's kernel).
-int rows_of(int64_t pairs, int64_t max_q, int g) {
-    const int64_t per_xcd = (pairs + kXcds - 1) / kXcds;
-    for (int rows = 256; rows > 32; rows /= 2)
-        if (per_xcd * ((max_q * g + rows - 1) / rows) >= kCus / kXcds) return rows;
-    return 32;
+// The splits' partial rows are merged by a wave per query row: O = (sum w acc + (sum w acc_r) . B_V[h]) / sum w l with w = 2^(m - max m)
+// (Eq. 4).  A workgroup is four query heads of one chunk token; a wave that took a token's heads in turn needed 100 us and more.
+__global__ __launch_bounds__(256) void merge_splits_kernel(PrefillArgs p, int r, int g) {
+    const int quads = p.hq / 4, quad = blockIdx.x % quads, at = blockIdx.x / quads;
+    const int a = at / p.reach, tok = at % p.reach;
+    const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
+    if (tok >= nq) return;
+    const int lane = threadIdx.x & 63, head = 4 * quad + uniform(threadIdx.x >> 6);
+    const int ad = r > 0 ? p.adapter_idx[a] : -1;
+    const int64_t n = (int64_t)p.hkv * D, step = (int64_t)p.n_agents * p.reach * p.hq * p.part_stride;
+    const float *rec = partial_row(p, 0, a, tok, head);
+    float m = kNegInf, l = 0.f;
+    if (lane < p.splits) {
+        m = rec[lane * step + p.part_stride - 4];
+        l = rec[lane * step + p.part_stride - 3];
+    }
+    const uint64_t live = __builtin_amdgcn_ballot_w64(!(m == kNegInf && l == 0.f));  // a split without keys has only m and l
+    float M = m;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x));
+    const float w = fast_exp2(m - (M == kNegInf ? 0.f : M));
+    float sum = w * l;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+    f32x2 o = {0.f, 0.f};
+    float low = 0.f;
+    const bool rank = ad >= 0 && lane < r;
+#pragma unroll 4
+    for (int i = 0; i < p.splits; ++i) {
+        const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
+        const bool on = (live >> i) & 1;
+        const f32x2 x = *reinterpret_cast<const f32x2 *>(rec + i * step + 2 * lane);
+        const float y = rank ? rec[i * step + D + lane] : 0.f;
+        o.x += on ? wi * x.x : 0.f;
+        o.y += on ? wi * x.y : 0.f;
+        low += on ? wi * y : 0.f;
+    }
+    if (ad >= 0) {
+        const uint16_t *bv = p.lora_b + ((int64_t)ad * 2 + 1) * r * n + (int64_t)(head / g) * D + 2 * lane;
+#pragma unroll 8
+        for (int rho = 0; rho < r; ++rho) {
+            const float x = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(low), rho));
+            const uint32_t b = *reinterpret_cast<const uint32_t *>(bv + rho * n);
+            o.x += x * bf16_lo(b);
+            o.y += x * bf16_hi(b);
+        }
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    *reinterpret_cast<uint32_t *>(p.out + ((int64_t)(q0 + tok) * p.hq + head) * D + 2 * lane) = pack_bf16(o.x * inv, o.y * inv);
 }
 
-template <int R, int G, int NRG>
+// Rows of a workgroup, and workgroups that share its keys.  An (agent, KV head) pair keeps to one XCD, so a grid takes as many passes
+// as the fullest XCD's workgroups over its compute units, and a grid that leaves half of them or more idle splits the keys over
+// them; its cost is the passes, times that of a key at so many rows, over the splits.  Fewer rows have to be 5 % better.
+// Time per key, grids of one pass (us per 1024 keys at 256 / 128 / 64 rows): rank 0 29.8 / 20.4 / 15.2, 16 36.4 / 25.7 /
+// 22.0, with RoPE 39.4 / 29.0 / 26.8, 64 with RoPE 67.4 / 47.7 / 67.0: rank 64 takes 128 rows at least.  (32 rows took as long as 64.)
+// Measured as the rule chooses (rows x splits) and beside it, us: four chunks of up to 250 over 35k, rank 16, 256 x 2 698, 128 x 1 877,
+// 256 x 3 856; one of 100 over 9k, rank 16, RoPE, 256 x 16 57, 64 x 1 237, 128 x 8 63, 64 x 8 89; one token of two agents over 60k,
+// 64 x 16 133, 64 x 1 1480, 64 x 32 128; eight of up to 1024 over 9k, 256 x 1 1577, 128 x 1 1861, 256 x 2 1722; two of 300 over 500 tokens,
+// rank 32, RoPE, 256 x 3 63, 128 x 1 59, 64 x 1 87.
+struct Grid {
+    int rows, splits;
+};
+Grid grid_of(int64_t pairs, int64_t max_q, int g, int r, int max_pages, bool split) {
+    constexpr int kXcdCus = kCus / kXcds, kSplitPages = 16;  // a split has 256 keys or more
+    constexpr struct {
+        int rows;
+        float cost;
+    } kForms[3] = {{256, 1.f}, {128, 0.72f}, {64, 0.6f}};
+    const int64_t per_xcd = (pairs + kXcds - 1) / kXcds;
+    const int most = split ? std::min(kXcdCus, std::max(1, max_pages / kSplitPages)) : 1;
+    Grid best = {256, 1};
+    float least = INFINITY;
+    for (const auto &f : kForms) {
+        if (f.rows < 128 && r > 32) continue;
+        const int64_t wgs = per_xcd * ((max_q * g + f.rows - 1) / f.rows);
+        const int splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, kXcdCus / wgs));
+        const float c = f.cost * (float)((wgs * splits + kXcdCus - 1) / kXcdCus) / splits;
+        if (c < least * 0.95f) least = c, best = {f.rows, splits};
+    }
+    return best;
+}
+constexpr int part_stride(int r) { return D + r + 4; }
+int64_t parts_bytes(const Grid &gr, int n_agents, int64_t max_q, int hq, int g, int r) {
+    const int64_t reach = (max_q * g + gr.rows - 1) / gr.rows * (gr.rows / g);
+    return (int64_t)gr.splits * n_agents * reach * hq * part_stride(r) * 4;
+}
+
+template <int R, int G>
 hipError_t launch(const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     const int pairs = (pa.n_agents * pa.hkv + kXcds - 1) / kXcds * kXcds;
     // timing events carry the kernel's own start and end timestamps (set by the launch)
     hipEvent_t e0 = ev ? static_cast<hipEvent_t>(ev[0]) : nullptr, e1 = ev ? static_cast<hipEvent_t>(ev[1]) : nullptr;
-    hipExtLaunchKernelGGL((prefill_fp8_kernel<R, G, NRG>), dim3(pairs * pa.blocks_per_agent_head), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
+    hipExtLaunchKernelGGL((prefill_fp8_kernel<R, G>), dim3(pairs * pa.blocks_per_agent_head * pa.splits), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
     return hipGetLastError();
 }
 
-template <int R, int G>
-hipError_t dispatch_rows(int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
-    switch (rows) {
-    case 64: return launch<R, G, 2>(pa, st, ev);
-    default: return launch<R, G, 1>(pa, st, ev);
-    }
-}
-
 template <int G>
-hipError_t dispatch(int r, int rows, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
+hipError_t dispatch(int r, const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     switch (r) {
-    case 0: return dispatch_rows<0, G>(rows, pa, st, ev);
-    case 8: return dispatch_rows<8, G>(rows, pa, st, ev);
-    case 16: return dispatch_rows<16, G>(rows, pa, st, ev);
-    case 32: return dispatch_rows<32, G>(rows, pa, st, ev);
-    case 64: return dispatch_rows<64, G>(rows, pa, st, ev);
+    case 0: return launch<0, G>(pa, st, ev);
+    case 8: return launch<8, G>(pa, st, ev);
+    case 16: return launch<16, G>(pa, st, ev);
+    case 32: return launch<32, G>(pa, st, ev);
     default: return hipErrorInvalidValue;
     }
 }
 
 }  // namespace
 
-hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, hipStream_t st, void *const *ev) {
-    const int rows = rows_of((int64_t)pa.n_agents * pa.hkv, max_q, g);
-    pa.blocks_per_agent_head = (int)((max_q * g + rows - 1) / rows);
-    if (rows >= 128) return launch_fp8_stream(r, g, rows, pa, st, ev);  // (measured beside that kernel)
-    return g == 4 ? dispatch<4>(r, rows, pa, st, ev) : dispatch<8>(r, rows, pa, st, ev);
+hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, void *workspace, size_t workspace_bytes, hipStream_t st, void *const *ev) {
+    const int64_t pairs = (int64_t)pa.n_agents * pa.hkv;
+    Grid gr = grid_of(pairs, max_q, g, r, pa.max_pages, true);
+    if (gr.splits > 1 && (!workspace || (int64_t)workspace_bytes < parts_bytes(gr, pa.n_agents, max_q, pa.hq, g, r)))
+        gr = grid_of(pairs, max_q, g, r, pa.max_pages, false);
+    pa.blocks_per_agent_head = (int)((max_q * g + gr.rows - 1) / gr.rows);
+    pa.splits = gr.splits;
+    pa.reach = pa.blocks_per_agent_head * (gr.rows / g);
+    pa.part_stride = part_stride(r);
+    pa.parts = static_cast<float *>(workspace);
+    void *first[2] = {ev ? ev[0] : nullptr, nullptr};
+    void *const *ev1 = gr.splits > 1 ? (ev ? first : nullptr) : ev;
+    hipError_t e = gr.rows >= 128 ? launch_fp8_stream(r, g, gr.rows, pa, st, ev1)
+                   : g == 4       ? dispatch<4>(r, pa, st, ev1)
+                                  : dispatch<8>(r, pa, st, ev1);
+    if (e != hipSuccess || gr.splits == 1) return e;
+    hipExtLaunchKernelGGL(merge_splits_kernel, dim3(pa.n_agents * pa.reach * (pa.hq / 4)), dim3(256), 0, st, nullptr, ev ? static_cast<hipEvent_t>(ev[1]) : nullptr, 0,
+                          pa, r, g);
+    return hipGetLastError();
 }
 
 }  // namespace fkvp
+
+extern "C" int64_t fkv_prefill_fp8_workspace_bytes(int32_t hq, int32_t hkv, int32_t r, int32_t n_agents, int32_t max_q, int32_t max_pages) {
+    const int g = hkv > 0 && hq > 0 && hq % hkv == 0 ? hq / hkv : 0;
+    if ((g != 4 && g != 8) || (r != 0 && r != 8 && r != 16 && r != 32 && r != 64) || n_agents < 1 || max_q < 1 || max_pages < 1) return 0;
+    const fkvp::Grid gr = fkvp::grid_of((int64_t)n_agents * hkv, max_q, g, r, max_pages, true);
+    return gr.splits > 1 ? fkvp::parts_bytes(gr, n_agents, max_q, hq, g, r) : 0;
+}

@@ -80,7 +80,7 @@ __device__ __forceinline__ void each(F &&f) {
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int R, int G, bool ROPE, int KG>
-__device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, int a, int h, int tok_begin) {
+__device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, int a, int h, int tok_begin, int split) {
     using S = Lay<R, KG>;
     constexpr int RT = S::RT, RTX = RT > 0 ? RT : 1, NRB = S::NRB, NRBX = NRB > 0 ? NRB : 1, TPW = S::ROWS / G, VT = S::VT;
     constexpr bool LROW = S::LROW;
@@ -93,8 +93,12 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     const int L = p.seq_lens[a], P0 = L - nq;
     const int ad = R > 0 ? p.adapter_idx[a] : -1;
     const int n_pages = (L + PS - 1) / PS;
-    const int last_pos = P0 + (tok_begin + TPW < nq ? tok_begin + TPW : nq) - 1;
-    const int n_tiles = last_pos / TILE_KEYS + 1;
+    const int tok_end = tok_begin + TPW < nq ? tok_begin + TPW : nq, last_pos = P0 + tok_end - 1;
+    // tiles of this split: n_tiles from t0 (tiles below are counted from t0)
+    const int all_tiles = last_pos / TILE_KEYS + 1, per_split = (all_tiles + p.splits - 1) / p.splits, t0 = split * per_split;
+    const int n_tiles = min(per_split, all_tiles - t0);
+    if (n_tiles <= 0) return empty_rows(p, split, a, h, G, tok_begin, tok_end);
+    const int key_t0 = t0 * TILE_KEYS, page_t0 = t0 * (TILE_KEYS / PS);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
     const int32_t *btb = p.base_bt + (int64_t)a * p.max_pages, *btr = R > 0 ? p.res_bt + (int64_t)a * p.max_pages : nullptr;
     const unsigned char *base = reinterpret_cast<const unsigned char *>(p.base_kv);
@@ -107,12 +111,12 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     uint32_t ke, ve;
     u32x4 c[RTX];
     f32x4 cs[2], sn[2];
-    auto page_of = [&](int tile) __attribute__((always_inline)) { return min(4 * tile + pw, n_pages - 1); };
+    auto page_of = [&](int tile) __attribute__((always_inline)) { return min(page_t0 + 4 * tile + pw, n_pages - 1); };
     // (buffer loads: a scalar base and one lane offset; lane addresses of 64 bits would be kept in registers for the launch)
     const int off16 = lane * 16, off8 = lane * 16 + half * 8, off_ve = PS + 4 * grp, off_ke = col;
     // Page ids of this wave's pages of 64 tiles, one per lane, and of the 64 after them: an id read where it is used would hold up the wave.
     auto ids = [&](int chunk, int &b, int &r) __attribute__((always_inline)) {
-        const int pg = min((64 * chunk + lane) * 4 + pw, n_pages - 1);
+        const int pg = min(page_t0 + (64 * chunk + lane) * 4 + pw, n_pages - 1);
         b = btb[pg];
         r = R > 0 ? btr[pg] : 0;
     };
@@ -184,7 +188,7 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             int lane = threadIdx.x & 63;
             asm("" : "+v"(lane));  // what follows from it is formed here, not kept for the launch
             const int col = lane & 15, grp = lane >> 4;
-            const int vis = L - (4 * tile + pw) * PS;  // tokens of the page inside the sequence
+            const int vis = L - (page_t0 + 4 * tile + pw) * PS;  // tokens of the page inside the sequence
             if (__builtin_expect(vis < PS, 0)) {  // unwritten values may be any bits, and meet zero weights
                 const int left = max(0, min(4, vis - 4 * grp));
                 const uint32_t m = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
@@ -484,17 +488,17 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
         i32x4 e = exps_of(0);
         request_angles(1, 0);
         step(F{}, T{}, F{}, N1{}, pa, pb, 0, 0, 0, 0, 0, 0, 0, 0, 0, g, 1);
-        step(T{}, T{}, F{}, N2{}, pa, pb, 0, e.x, e.y, 0, 1, 0, 0, 0, 0, g, 1);
+        step(T{}, T{}, F{}, N2{}, pa, pb, key_t0, e.x, e.y, 0, 1, 0, 0, 0, 0, g, 1);
         for (int u = 1; u < n_tiles; ++u) {
             lds_fence_barrier();  // (not one that waits for the loads in flight) tile u is staged, tile u - 1's keys and tile u - 2's values are read
             const i32x4 en = exps_of(u);
             request_angles(u + 1, 0);
-            step(T{}, T{}, T{}, N1{}, pb, pa, (u - 1) * TILE_KEYS + 32, e.z, e.w, u, 0, u - 1, 0, u - 1, 1, g, u + 1);
-            step(T{}, T{}, T{}, N2{}, pa, pb, u * TILE_KEYS, en.x, en.y, u, 1, u - 1, 1, u, 0, g, u + 1);
+            step(T{}, T{}, T{}, N1{}, pb, pa, key_t0 + (u - 1) * TILE_KEYS + 32, e.z, e.w, u, 0, u - 1, 0, u - 1, 1, g, u + 1);
+            step(T{}, T{}, T{}, N2{}, pa, pb, key_t0 + u * TILE_KEYS, en.x, en.y, u, 1, u - 1, 1, u, 0, g, u + 1);
             e = en;
         }
         // the last tile's second half, and its values
-        step(T{}, F{}, T{}, N0{}, pb, pa, (n_tiles - 1) * TILE_KEYS + 32, e.z, e.w, 0, 0, n_tiles - 1, 0, n_tiles - 1, 1, g, 0);
+        step(T{}, F{}, T{}, N0{}, pb, pa, key_t0 + (n_tiles - 1) * TILE_KEYS + 32, e.z, e.w, 0, 0, n_tiles - 1, 0, n_tiles - 1, 1, g, 0);
         step(F{}, F{}, T{}, N0{}, pa, pb, 0, 0, 0, 0, 0, n_tiles - 1, 1, 0, 0, g, 0);
     } else {
         // Key group kg takes half kg of every tile, one step per tile: values of tile u - 2, weights of u - 1, scores of u.  (Before there
@@ -508,12 +512,12 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             lds_fence_barrier();  // tile u is staged, tile u - 1's keys and tile u - 3's values are read
             const u32x2 en = pages_of(u);
             request_angles(u + 1, 0);
-            step(T{}, T{}, T{}, N3{}, pa, pb, (u - 1) * TILE_KEYS + 32 * kg, e.x, e.y, u, kg, max(u - 2, 0), kg, u - 1, kg, g, u + 1);
+            step(T{}, T{}, T{}, N3{}, pa, pb, key_t0 + (u - 1) * TILE_KEYS + 32 * kg, e.x, e.y, u, kg, max(u - 2, 0), kg, u - 1, kg, g, u + 1);
             pa[0] = pb[0];
             pa[1] = pb[1];
             e = en;
         }
-        step(T{}, F{}, T{}, N0{}, pa, pb, (n_tiles - 1) * TILE_KEYS + 32 * kg, e.x, e.y, 0, 0, max(n_tiles - 2, 0), kg, n_tiles - 1, kg, g, 0);
+        step(T{}, F{}, T{}, N0{}, pa, pb, key_t0 + (n_tiles - 1) * TILE_KEYS + 32 * kg, e.x, e.y, 0, 0, max(n_tiles - 2, 0), kg, n_tiles - 1, kg, g, 0);
         step(F{}, F{}, T{}, N0{}, pb, pa, 0, 0, 0, 0, 0, n_tiles - 1, kg, 0, 0, g, 0);
     }
     __syncthreads();
@@ -546,12 +550,32 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
                 for (int j = 0; j < 4; ++j) racc[i / 4][4 * (i % 4) + j] = racc[i / 4][4 * (i % 4) + j] * w0 + x[j] * w1;
             }
             lsum = lsum * w0 + ml.y * w1;
+            m_run = M;
         }
         __syncthreads();
     }
 
     // ---- epilogue: O = (acc + acc_r . B_V[h]) / l; lane: row r32, dims 32 b + 8 (i / 4) + 4 hh + i % 4 ----
     const float l_run = LROW ? __shfl(racc[0][8], r32) : lsum + __shfl_xor(lsum, 32);
+    if (p.splits > 1) {  // this split's partial rows
+        if (kg > 0 || row_tok < 0) return;
+        float *rec = partial_row(p, split, a, row_tok, h * G + (rg * 32 + r32) % G);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4 *>(rec + 32 * b + 8 * i + 4 * hh) =
+                    f32x4{oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
+#pragma unroll
+        for (int b = 0; b < NRB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (32 * b + 8 * i + 4 * hh < R)
+                    *reinterpret_cast<f32x4 *>(rec + D + 32 * b + 8 * i + 4 * hh) =
+                        f32x4{racc[b][4 * i], racc[b][4 * i + 1], racc[b][4 * i + 2], racc[b][4 * i + 3]};
+        if (hh == 0) *reinterpret_cast<f32x4 *>(rec + p.part_stride - 4) = f32x4{m_run, l_run, 0.f, 0.f};
+        return;
+    }
     if constexpr (R > 0) {
         float *bv = reinterpret_cast<float *>(lds), *acc = bv + R * D;
         const uint16_t *src = p.lora_b + ((int64_t)ad * 2 + 1) * R * n + (int64_t)h * D;
@@ -601,15 +625,15 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_stream_kernel(Prefi
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Lay<R, KG>::BYTES > Lay<0, KG>::BYTES ? Lay<R, KG>::BYTES : Lay<0, KG>::BYTES];
     const int bpa = p.blocks_per_agent_head;
     const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
-    const int pair = (local / bpa) * kXcds + xcd, qb = local % bpa;
+    const int pair = local / (bpa * p.splits) * kXcds + xcd, qb = local % bpa, split = local / bpa % p.splits;
     if (pair >= p.n_agents * p.hkv) return;
     const int a = pair / p.hkv, h = pair % p.hkv;
     const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
     const int tok_begin = qb * TPW;
-    if (qb == bpa - 1 && nq > bpa * TPW) poison_unreached_rows(p, q0, nq, h, G, bpa * TPW);
+    if (qb == bpa - 1 && split == 0 && nq > bpa * TPW) poison_unreached_rows(p, q0, nq, h, G, bpa * TPW);
     if (tok_begin >= nq) return;
-    if (R > 0 && p.adapter_idx[a] >= 0) block<R, G, ROPE, KG>(p, lds, a, h, tok_begin);
-    else block<0, G, false, KG>(p, lds, a, h, tok_begin);
+    if (R > 0 && p.adapter_idx[a] >= 0) block<R, G, ROPE, KG>(p, lds, a, h, tok_begin, split);
+    else block<0, G, false, KG>(p, lds, a, h, tok_begin, split);
 }
 
 template <int R, int G, bool ROPE, int KG>
@@ -617,7 +641,7 @@ hipError_t launch(const PrefillArgs &pa, hipStream_t st, void *const *ev) {
     const int pairs = (pa.n_agents * pa.hkv + kXcds - 1) / kXcds * kXcds;
     // timing events carry the kernel's own start and end timestamps (set by the launch)
     hipEvent_t e0 = ev ? static_cast<hipEvent_t>(ev[0]) : nullptr, e1 = ev ? static_cast<hipEvent_t>(ev[1]) : nullptr;
-    hipExtLaunchKernelGGL((prefill_fp8_stream_kernel<R, G, ROPE, KG>), dim3(pairs * pa.blocks_per_agent_head), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
+    hipExtLaunchKernelGGL((prefill_fp8_stream_kernel<R, G, ROPE, KG>), dim3(pairs * pa.blocks_per_agent_head * pa.splits), dim3(64 * WAVES), 0, st, e0, e1, 0, pa);
     return hipGetLastError();
 }
 

@@ -483,10 +483,25 @@ def residual_attention_decode_fp8(args: N.fkv_attn_args, plan: DecodePlan, strea
           "fkv_residual_attention_decode_fp8")
 
 
+def prefill_fp8_workspace_bytes(hq: int, hkv: int, r: int, n_agents: int, max_q: int, max_pages: int) -> int:
+    """fkv_prefill_fp8_workspace_bytes: scratch with which the 8-bit prefill splits long contexts (0: it does not)."""
+    return N.fkv_prefill_fp8_workspace_bytes(hq, hkv, r, n_agents, max_q, max_pages)
+
+
 def residual_attention_prefill_fp8(args: N.fkv_attn_args, stream=None) -> None:
-    """fkv_residual_attention_prefill_fp8: base_kv of the arguments is an 8-bit pool."""
-    _pool_format(args, True, "fkv_residual_attention_prefill_fp8")
-    check(N.fkv_residual_attention_prefill_fp8(ctypes.byref(args), _stream(stream)), "fkv_residual_attention_prefill_fp8")
+    """fkv_residual_attention_prefill_fp8: base_kv of the arguments is an 8-bit pool.  Scratch for the call is args.workspace if
+    that is large enough (prefill_fp8_workspace_bytes), else it comes from torch's allocator."""
+    who = "fkv_residual_attention_prefill_fp8"
+    _pool_format(args, True, who)
+    need = N.fkv_prefill_fp8_workspace_bytes(args.hq, args.hkv, args.r, args.n_agents, args.max_q_per_agent or args.n_q, args.max_pages)
+    if need > (args.workspace_bytes if args.workspace else 0):
+        scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+        if stream is not None and _stream(stream) != _stream(None):
+            scratch.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
+        mine = N.fkv_attn_args.from_buffer_copy(args)
+        mine.workspace, mine.workspace_bytes = scratch.data_ptr(), need
+        args = mine
+    check(N.fkv_residual_attention_prefill_fp8(ctypes.byref(args), _stream(stream)), who)
 
 
 def residual_attention_prefill(args: N.fkv_attn_args, stream=None) -> None:

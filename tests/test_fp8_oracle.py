@@ -159,6 +159,19 @@ def test_attention_refusals_without_a_gpu(kw):
         assert f"fkv_residual_attention_{name}_fp8" in N.fkv_last_error().decode()
 
 
+def test_prefill_workspace():
+    # the smaller the grid the more workgroups share a row's keys; none where the grid fills the GPU or contexts are short
+    need = lambda *a: rt.prefill_fp8_workspace_bytes(*a)  # noqa: E731
+    assert need(32, 8, 16, 1, 1, 4096) == 32 * 16 * 32 * (128 + 16 + 4) * 4  # splits, tokens of a workgroup, heads, floats of a record
+    assert need(32, 8, 16, 1, 1, 31) == 0 and need(32, 8, 16, 64, 4096, 4096) == 0
+    assert need(32, 8, 16, 1, 1, 64) == need(32, 8, 16, 1, 1, 4096) * 4 // 32
+    for bad in ((32, 8, 24, 1, 1, 64), (32, 5, 16, 1, 1, 64), (8, 8, 16, 1, 1, 64), (32, 8, 16, 0, 1, 64), (32, 8, 16, 1, 0, 64), (32, 8, 16, 1, 1, 0),
+                (0, 0, 0, 0, 0, 0), (-32, -8, 16, 1, 1, 64)):
+        assert need(*bad) == 0
+    assert N.fkv_residual_attention_prefill_fp8(ctypes.byref(_attn(workspace=4104)), None) == N.FKV_ERR_INVALID
+    assert "workspace" in N.fkv_last_error().decode()
+
+
 def test_null_arguments_are_refused():
     assert N.fkv_residual_attention_prefill_fp8(None, None) == N.FKV_ERR_INVALID
     assert N.fkv_residual_attention_decode_fp8(None, None, None) == N.FKV_ERR_INVALID

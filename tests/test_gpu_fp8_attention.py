@@ -10,11 +10,14 @@ product: K, or its low-rank part) -- a score error of D moves a weight by a fact
 normalisation.  fp32 sums add less than 1 % of that.  Beside it, since roundings are not all at their worst, the 2-norm of the
 error is at most 1e-2 of the result's (the bar of the bf16 path's tests).  Unwritten slots hold NaN codes, exponent byte 255 and NaN rCache rows throughout.
 """
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import fp8_cache as o
+from paper_2604_06370_amd import _native as N
 from paper_2604_06370_amd import runtime as rt
 from paper_2604_06370_amd import workloads as W
 from paper_2604_06370_amd.driver import LoadedWorkload
@@ -253,6 +256,82 @@ def test_prefill_middle_grids(r, rope):
     """Grids that fill the compute units with 128 rows per workgroup and not with 256: contexts of one tile to many, whole and partial."""
     p = Problem(14, [1000, 63, 250, 4130], 0, 32, 8, r, rope, rows=[250, 63, 250, 249], bare=(0,))
     p.check(p.prefill())
+
+
+def _without_workspace(p, max_q=0):
+    """The C call without scratch: one workgroup passes over all keys of a row."""
+    out = torch.full_like(p.q, 9.0)
+    args = p.args(out, q_indptr=p.indptr, n_q=sum(p.rows), max_q_per_agent=max_q or max(p.rows))
+    N.check(N.fkv_residual_attention_prefill_fp8(ctypes.byref(args), torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("r,rope", RANKS)
+@pytest.mark.parametrize("hq,hkv,lens,rows", [
+    (64, 8, [9001], [1]),                        # one row per head over a long context, a workgroup per 256 keys
+    (4, 1, [3000, 20, 1, 517], [4, 20, 1, 33]),  # contexts shorter than the splits: most of them are empty
+    (32, 8, [4133, 2000], [64, 250]),            # 256 rows, a chunk that ends before the last block
+])
+def test_prefill_splits_long_contexts(hq, hkv, lens, rows, r, rope):
+    p = Problem(15, lens, 0, hq, hkv, r, rope, rows=rows, bare=(0,) if len(lens) == 4 else ())
+    width = p.base.shape[1]
+    assert rt.prefill_fp8_workspace_bytes(hq, hkv, r, len(lens), max(rows), width) > 0
+    p.check(p.prefill())
+    p.check(_without_workspace(p))
+
+
+def test_prefill_splits_with_the_callers_workspace():
+    p = Problem(16, [5000, 700], 0, 32, 8, 16, True, rows=[3, 40])
+    want, whole = p.prefill(), _without_workspace(p)
+    need = rt.prefill_fp8_workspace_bytes(32, 8, 16, 2, 40, p.base.shape[1])
+    kw = dict(q_indptr=p.indptr, n_q=43, max_q_per_agent=40)
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")  # NaN, and a guard behind it
+    out = torch.zeros_like(p.q)
+    rt.residual_attention_prefill_fp8(p.args(out, workspace=ws[:need], **kw))
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and bool((ws[need:] == 255).all()) and not bool((ws[:need] == 255).all())
+    args = p.args(out, workspace=ws[:need - 16], **kw)  # too small for the C call: no split
+    N.check(N.fkv_residual_attention_prefill_fp8(ctypes.byref(args), torch.cuda.current_stream().cuda_stream))
+    torch.cuda.synchronize()
+    assert torch.equal(out, whole) and not torch.equal(out, want)
+
+
+def test_prefill_splits_keep_unreached_rows_nan():
+    p = Problem(17, [2000, 900], 0, 32, 8, 16, False, rows=[200, 20])
+    out = p.prefill(max_q=64)
+    ref, bound = p.reference()
+    reached = torch.ones(220, dtype=torch.bool, device="cuda")
+    reached[64:200] = False
+    assert torch.isnan(out[~reached].float()).all()
+    assert ((out.double() - ref).abs() <= bound)[reached].all()
+
+
+def test_prefill_splits_in_a_graph_and_on_two_streams():
+    ps = [Problem(18 + i, [6000, 333], 0, 32, 8, 16, i == 1, rows=[5, 60]) for i in range(2)]
+    want = [p.prefill() for p in ps]
+    outs = [torch.zeros_like(p.q) for p in ps]
+    args = [p.args(out, q_indptr=p.indptr, n_q=65, max_q_per_agent=60) for p, out in zip(ps, outs)]
+    streams = [torch.cuda.Stream() for _ in ps]
+    for _ in range(3):  # scratch of calls in flight at once is not shared
+        for out in outs:
+            out.zero_()
+        torch.cuda.synchronize()
+        for a, s in zip(args, streams):
+            rt.residual_attention_prefill_fp8(a, s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, w) for out, w in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for a in args:
+            rt.residual_attention_prefill_fp8(a)
+    for _ in range(4):
+        for out in outs:
+            out.zero_()
+        graph.replay()
+        eager = ps[0].prefill()
+        torch.cuda.synchronize()
+        assert torch.equal(eager, want[0]) and all(torch.equal(out, w) for out, w in zip(outs, want))
 
 
 @pytest.mark.parametrize("r", [0, 16])
