@@ -475,8 +475,9 @@ fkv_status fkv_page_copy_list_fp8(const fkv_page_copy *copies, int32_t n, void *
 
 /* ResidualAttention over an 8-bit base pool: fkv_residual_attention_decode and _prefill with args->base_kv
  * pointing to one (16-byte aligned).  The same shapes, plans (a plan serves either format), workspaces, block tables,
- * residual pool, streams and errors; K_base and V_base are the values the cache stands for, the products take them
- * exactly (in bf16, as the queries and weights are), sums and softmax statistics are fp32. */
+ * residual pool, streams and errors; K_base and V_base are the values the cache stands for.  Decode's products take them
+ * exactly (in bf16, as its queries and weights are); prefill's take the values so, and keys and queries in fp16 relative to the largest
+ * of their page and row.  Sums and softmax statistics are fp32. */
 fkv_status fkv_residual_attention_decode_fp8(const fkv_attn_args *args, const fkv_plan *plan, void *stream);
 fkv_status fkv_residual_attention_prefill_fp8(const fkv_attn_args *args, void *stream);
 

@@ -631,6 +631,7 @@ hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, void *workspa
 extern "C" int64_t fkv_prefill_fp8_workspace_bytes(int32_t hq, int32_t hkv, int32_t r, int32_t n_agents, int32_t max_q, int32_t max_pages) {
     const int g = hkv > 0 && hq > 0 && hq % hkv == 0 ? hq / hkv : 0;
     if ((g != 4 && g != 8) || (r != 0 && r != 8 && r != 16 && r != 32 && r != 64) || n_agents < 1 || max_q < 1 || max_pages < 1) return 0;
+    if ((int64_t)n_agents * hkv >= 1 << 24 || max_q >= 1 << 28) return 0;  // (no split there, and their products stay in 64 bits)
     const fkvp::Grid gr = fkvp::grid_of((int64_t)n_agents * hkv, max_q, g, r, max_pages, true);
     return gr.splits > 1 ? fkvp::parts_bytes(gr, n_agents, max_q, hq, g, r) : 0;
 }

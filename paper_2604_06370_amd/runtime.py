@@ -495,9 +495,10 @@ def residual_attention_prefill_fp8(args: N.fkv_attn_args, stream=None) -> None:
     _pool_format(args, True, who)
     need = N.fkv_prefill_fp8_workspace_bytes(args.hq, args.hkv, args.r, args.n_agents, args.max_q_per_agent or args.n_q, args.max_pages)
     if need > (args.workspace_bytes if args.workspace else 0):
-        scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
-        if stream is not None and _stream(stream) != _stream(None):
-            scratch.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
+        # from the pool of the stream that uses it: a block of another stream's may still be in use there
+        own = stream if stream is None or isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream))
+        with torch.cuda.stream(own):
+            scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
         mine = N.fkv_attn_args.from_buffer_copy(args)
         mine.workspace, mine.workspace_bytes = scratch.data_ptr(), need
         args = mine

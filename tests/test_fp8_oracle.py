@@ -166,7 +166,7 @@ def test_prefill_workspace():
     assert need(32, 8, 16, 1, 1, 31) == 0 and need(32, 8, 16, 64, 4096, 4096) == 0
     assert need(32, 8, 16, 1, 1, 64) == need(32, 8, 16, 1, 1, 4096) * 4 // 32
     for bad in ((32, 8, 24, 1, 1, 64), (32, 5, 16, 1, 1, 64), (8, 8, 16, 1, 1, 64), (32, 8, 16, 0, 1, 64), (32, 8, 16, 1, 0, 64), (32, 8, 16, 1, 1, 0),
-                (0, 0, 0, 0, 0, 0), (-32, -8, 16, 1, 1, 64)):
+                (0, 0, 0, 0, 0, 0), (-32, -8, 16, 1, 1, 64), (32, 8, 16, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1)):
         assert need(*bad) == 0
     assert N.fkv_residual_attention_prefill_fp8(ctypes.byref(_attn(workspace=4104)), None) == N.FKV_ERR_INVALID
     assert "workspace" in N.fkv_last_error().decode()

@@ -334,6 +334,30 @@ def test_prefill_splits_in_a_graph_and_on_two_streams():
         assert torch.equal(eager, want[0]) and all(torch.equal(out, w) for out, w in zip(outs, want))
 
 
+@pytest.mark.parametrize("raw", [False, True])
+def test_prefill_scratch_belongs_to_its_stream(raw):
+    """Memory freed on the current stream with work pending there is not the scratch of a call on another stream."""
+    p = Problem(21, [6000], 0, 32, 8, 16, False, rows=[5])
+    want, out = p.prefill(), torch.zeros_like(p.q)
+    args = p.args(out, q_indptr=p.indptr, n_q=5, max_q_per_agent=5)
+    need = rt.prefill_fp8_workspace_bytes(32, 8, 16, 1, 5, p.base.shape[1])
+    side, a = torch.cuda.Stream(), torch.full((4096, 4096), 1e-4, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    for _ in range(3):
+        held = [torch.empty(need, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        for _ in range(8):
+            a = a @ a * 1e-3
+        for x in held:
+            x.fill_(255)
+        del held, x
+        rt.residual_attention_prefill_fp8(args, side.cuda_stream if raw else side)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        out.zero_()
+        torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("r", [0, 16])
 def test_prefill_understated_rows_are_nan(r):
     p = Problem(13, [400, 300], 0, 32, 8, r, False, rows=[200, 20])
