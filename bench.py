@@ -42,7 +42,7 @@ HBM_PEAK_GBS = 8000.0
 MFMA_BF16_PEAK_TFLOPS = 2500.0  # dense bf16 matrix-core peak of MI355X
 ROOT = os.path.dirname(os.path.abspath(__file__))
 TRAFFIC_SUMMARY = os.path.join(ROOT, "profiles", "decode_llama3-8b-16agents-32k-shared_hbm_traffic.md")
-KERNEL_SOURCE = os.path.join(ROOT, "paper_2604_06370_amd", "csrc", "decode.hip")
+KERNEL_SOURCE = os.path.join(ROOT, "paper_2604_06370_amd", "csrc", "decode_kernels.hpp")
 
 
 def counter_traffic(rope: bool, workload: str, pages_per_split: int):
