@@ -79,6 +79,19 @@ __device__ __forceinline__ void each(F &&f) {
 }
 __device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
 
+// A workgroup's place in the grid.
+struct Place {
+    int a, h, qb, split;
+    __device__ __forceinline__ Place(const PrefillArgs &p, int block) {
+        const int bpa = p.blocks_per_agent_head, local = block / kXcds;
+        const int pair = local / (bpa * p.splits) * kXcds + block % kXcds;
+        a = pair / p.hkv;
+        h = pair % p.hkv;
+        qb = local % bpa;
+        split = local / bpa % p.splits;
+    }
+};
+
 template <int R, int G, bool ROPE, int KG>
 __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, int a, int h, int tok_begin, int split) {
     using S = Lay<R, KG>;
@@ -90,17 +103,19 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     const int hkv = p.hkv;
     const int64_t n = (int64_t)hkv * D;
     const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
-    const int L = p.seq_lens[a], P0 = L - nq;
+    int L = p.seq_lens[a], P0 = L - nq;
     const int ad = R > 0 ? p.adapter_idx[a] : -1;
-    const int n_pages = (L + PS - 1) / PS;
     const int tok_end = tok_begin + TPW < nq ? tok_begin + TPW : nq, last_pos = P0 + tok_end - 1;
-    // tiles of this split: n_tiles from t0 (tiles below are counted from t0)
     const int all_tiles = last_pos / TILE_KEYS + 1, per_split = (all_tiles + p.splits - 1) / p.splits, t0 = split * per_split;
-    const int n_tiles = min(per_split, all_tiles - t0);
+    const int n_tiles = min(per_split, all_tiles - t0);  // of this split
     if (n_tiles <= 0) return empty_rows(p, split, a, h, G, tok_begin, tok_end);
-    const int key_t0 = t0 * TILE_KEYS, page_t0 = t0 * (TILE_KEYS / PS);
+    // from here on tiles, pages and positions are counted from the split's first
+    const int page_t0 = t0 * (TILE_KEYS / PS);
+    L -= t0 * TILE_KEYS;
+    P0 -= t0 * TILE_KEYS;
+    const int n_pages = (L + PS - 1) / PS;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds;
-    const int32_t *btb = p.base_bt + (int64_t)a * p.max_pages, *btr = R > 0 ? p.res_bt + (int64_t)a * p.max_pages : nullptr;
+    const int32_t *btb = p.base_bt + (int64_t)a * p.max_pages + page_t0, *btr = R > 0 ? p.res_bt + (int64_t)a * p.max_pages + page_t0 : nullptr;
     const unsigned char *base = reinterpret_cast<const unsigned char *>(p.base_kv);
     int *page_exp = reinterpret_cast<int *>(lds + S::E_OFF);  // [2 tiles][page]
 
@@ -111,12 +126,12 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     uint32_t ke, ve;
     u32x4 c[RTX];
     f32x4 cs[2], sn[2];
-    auto page_of = [&](int tile) __attribute__((always_inline)) { return min(page_t0 + 4 * tile + pw, n_pages - 1); };
+    auto page_of = [&](int tile) __attribute__((always_inline)) { return min(4 * tile + pw, n_pages - 1); };
     // (buffer loads: a scalar base and one lane offset; lane addresses of 64 bits would be kept in registers for the launch)
     const int off16 = lane * 16, off8 = lane * 16 + half * 8, off_ve = PS + 4 * grp, off_ke = col;
     // Page ids of this wave's pages of 64 tiles, one per lane, and of the 64 after them: an id read where it is used would hold up the wave.
     auto ids = [&](int chunk, int &b, int &r) __attribute__((always_inline)) {
-        const int pg = min(page_t0 + (64 * chunk + lane) * 4 + pw, n_pages - 1);
+        const int pg = min((64 * chunk + lane) * 4 + pw, n_pages - 1);
         b = btb[pg];
         r = R > 0 ? btr[pg] : 0;
     };
@@ -151,7 +166,7 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     };
     auto request_angles = [&](int tile, int w) __attribute__((always_inline)) {  // of frequency tile 2 half + w
         if constexpr (ROPE) {
-            const int64_t at = (int64_t)page_of(tile) * (PS * D / 2 * 4);
+            const int64_t at = (int64_t)(page_t0 + page_of(tile)) * (PS * D / 2 * 4);
             const i32x4 rc = block_rsrc(reinterpret_cast<uint64_t>(p.rope_cos) + at, PS * D / 2 * 4);
             const i32x4 rs = block_rsrc(reinterpret_cast<uint64_t>(p.rope_sin) + at, PS * D / 2 * 4);
             cs[w] = __builtin_bit_cast(f32x4, buf_load16_at(rc, off16, 2048 * half + 1024 * w));
@@ -188,7 +203,7 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             int lane = threadIdx.x & 63;
             asm("" : "+v"(lane));  // what follows from it is formed here, not kept for the launch
             const int col = lane & 15, grp = lane >> 4;
-            const int vis = L - (page_t0 + 4 * tile + pw) * PS;  // tokens of the page inside the sequence
+            const int vis = L - (4 * tile + pw) * PS;  // tokens of the page inside the sequence
             if (__builtin_expect(vis < PS, 0)) {  // unwritten values may be any bits, and meet zero weights
                 const int left = max(0, min(4, vis - 4 * grp));
                 const uint32_t m = left == 4 ? 0xffffffffu : (1u << (8 * left)) - 1u;
@@ -488,17 +503,17 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
         i32x4 e = exps_of(0);
         request_angles(1, 0);
         step(F{}, T{}, F{}, N1{}, pa, pb, 0, 0, 0, 0, 0, 0, 0, 0, 0, g, 1);
-        step(T{}, T{}, F{}, N2{}, pa, pb, key_t0, e.x, e.y, 0, 1, 0, 0, 0, 0, g, 1);
+        step(T{}, T{}, F{}, N2{}, pa, pb, 0, e.x, e.y, 0, 1, 0, 0, 0, 0, g, 1);
         for (int u = 1; u < n_tiles; ++u) {
             lds_fence_barrier();  // (not one that waits for the loads in flight) tile u is staged, tile u - 1's keys and tile u - 2's values are read
             const i32x4 en = exps_of(u);
             request_angles(u + 1, 0);
-            step(T{}, T{}, T{}, N1{}, pb, pa, key_t0 + (u - 1) * TILE_KEYS + 32, e.z, e.w, u, 0, u - 1, 0, u - 1, 1, g, u + 1);
-            step(T{}, T{}, T{}, N2{}, pa, pb, key_t0 + u * TILE_KEYS, en.x, en.y, u, 1, u - 1, 1, u, 0, g, u + 1);
+            step(T{}, T{}, T{}, N1{}, pb, pa, (u - 1) * TILE_KEYS + 32, e.z, e.w, u, 0, u - 1, 0, u - 1, 1, g, u + 1);
+            step(T{}, T{}, T{}, N2{}, pa, pb, u * TILE_KEYS, en.x, en.y, u, 1, u - 1, 1, u, 0, g, u + 1);
             e = en;
         }
         // the last tile's second half, and its values
-        step(T{}, F{}, T{}, N0{}, pb, pa, key_t0 + (n_tiles - 1) * TILE_KEYS + 32, e.z, e.w, 0, 0, n_tiles - 1, 0, n_tiles - 1, 1, g, 0);
+        step(T{}, F{}, T{}, N0{}, pb, pa, (n_tiles - 1) * TILE_KEYS + 32, e.z, e.w, 0, 0, n_tiles - 1, 0, n_tiles - 1, 1, g, 0);
         step(F{}, F{}, T{}, N0{}, pa, pb, 0, 0, 0, 0, 0, n_tiles - 1, 1, 0, 0, g, 0);
     } else {
         // Key group kg takes half kg of every tile, one step per tile: values of tile u - 2, weights of u - 1, scores of u.  (Before there
@@ -512,12 +527,12 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
             lds_fence_barrier();  // tile u is staged, tile u - 1's keys and tile u - 3's values are read
             const u32x2 en = pages_of(u);
             request_angles(u + 1, 0);
-            step(T{}, T{}, T{}, N3{}, pa, pb, key_t0 + (u - 1) * TILE_KEYS + 32 * kg, e.x, e.y, u, kg, max(u - 2, 0), kg, u - 1, kg, g, u + 1);
+            step(T{}, T{}, T{}, N3{}, pa, pb, (u - 1) * TILE_KEYS + 32 * kg, e.x, e.y, u, kg, max(u - 2, 0), kg, u - 1, kg, g, u + 1);
             pa[0] = pb[0];
             pa[1] = pb[1];
             e = en;
         }
-        step(T{}, F{}, T{}, N0{}, pa, pb, key_t0 + (n_tiles - 1) * TILE_KEYS + 32 * kg, e.x, e.y, 0, 0, max(n_tiles - 2, 0), kg, n_tiles - 1, kg, g, 0);
+        step(T{}, F{}, T{}, N0{}, pa, pb, (n_tiles - 1) * TILE_KEYS + 32 * kg, e.x, e.y, 0, 0, max(n_tiles - 2, 0), kg, n_tiles - 1, kg, g, 0);
         step(F{}, F{}, T{}, N0{}, pb, pa, 0, 0, 0, 0, 0, n_tiles - 1, kg, 0, 0, g, 0);
     }
     __syncthreads();
@@ -557,9 +572,13 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
 
     // ---- epilogue: O = (acc + acc_r . B_V[h]) / l; lane: row r32, dims 32 b + 8 (i / 4) + 4 hh + i % 4 ----
     const float l_run = LROW ? __shfl(racc[0][8], r32) : lsum + __shfl_xor(lsum, 32);
+    // what the epilogue takes is derived again, from a copy that the compiler takes for another: kept over the loop it would be spilled
+    int block_id = blockIdx.x;
+    asm volatile("" : "+s"(block_id));
+    const Place at(p, block_id);
     if (p.splits > 1) {  // this split's partial rows
         if (kg > 0 || row_tok < 0) return;
-        float *rec = partial_row(p, split, a, row_tok, h * G + (rg * 32 + r32) % G);
+        float *rec = partial_row(p, at.split, at.a, row_tok, at.h * G + (rg * 32 + r32) % G);
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -578,7 +597,8 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     }
     if constexpr (R > 0) {
         float *bv = reinterpret_cast<float *>(lds), *acc = bv + R * D;
-        const uint16_t *src = p.lora_b + ((int64_t)ad * 2 + 1) * R * n + (int64_t)h * D;
+        const int64_t n = (int64_t)p.hkv * D;
+        const uint16_t *src = p.lora_b + ((int64_t)p.adapter_idx[at.a] * 2 + 1) * R * n + (int64_t)at.h * D;
         for (int e = threadIdx.x; e < R * D / 2; e += 64 * WAVES) {
             const uint32_t w = *reinterpret_cast<const uint32_t *>(src + (int64_t)(e / (D / 2)) * n + 2 * (e % (D / 2)));
             bv[2 * e] = bf16_lo(w);
@@ -608,7 +628,7 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     }
     if (kg == 0 && row_tok >= 0) {
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-        uint16_t *o = p.out + ((int64_t)(q0 + row_tok) * p.hq + h * G + (rg * 32 + r32) % G) * D;
+        uint16_t *o = p.out + ((int64_t)(p.q_indptr[at.a] + row_tok) * p.hq + at.h * G + (rg * 32 + r32) % G) * D;
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -623,13 +643,12 @@ template <int R, int G, bool ROPE, int KG>
 __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_stream_kernel(PrefillArgs p) {
     constexpr int TPW = Lay<R, KG>::ROWS / G;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[Lay<R, KG>::BYTES > Lay<0, KG>::BYTES ? Lay<R, KG>::BYTES : Lay<0, KG>::BYTES];
-    const int bpa = p.blocks_per_agent_head;
-    const int xcd = blockIdx.x % kXcds, local = blockIdx.x / kXcds;
-    const int pair = local / (bpa * p.splits) * kXcds + xcd, qb = local % bpa, split = local / bpa % p.splits;
-    if (pair >= p.n_agents * p.hkv) return;
-    const int a = pair / p.hkv, h = pair % p.hkv;
+    const Place at(p, blockIdx.x);
+    const int a = at.a, h = at.h, qb = at.qb, split = at.split;
+    if (a >= p.n_agents) return;
     const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
     const int tok_begin = qb * TPW;
+    const int bpa = p.blocks_per_agent_head;
     if (qb == bpa - 1 && split == 0 && nq > bpa * TPW) poison_unreached_rows(p, q0, nq, h, G, bpa * TPW);
     if (tok_begin >= nq) return;
     if (R > 0 && p.adapter_idx[a] >= 0) block<R, G, ROPE, KG>(p, lds, a, h, tok_begin, split);
