@@ -15,12 +15,13 @@ struct PrefillArgs {
     int32_t n_agents, hq, hkv, max_pages, blocks_per_agent_head;
     float scale_log2;
     int32_t rope_rows;  // positions the RoPE tables hold
-    // 8-bit pages: each agent's keys are split over `splits` workgroups, which leave partial rows in `parts`, records of `part_stride`
-    // floats [split][agent][token of the chunk, of `reach`][query head]: acc[128], acc_r[R], m and l at part_stride - 4
+    // 8-bit pages: each agent's keys are split over `splits` workgroups, which leave partial rows in `parts`, records of kPartFloats
+    // floats [split][agent][token of the chunk, of `reach`][query head]: acc[128] (with acc_r . B_V[h]), m, l, and two to align
     float *parts;
-    int32_t splits, reach, part_stride;
+    int32_t splits, reach;
 };
 
+constexpr int kPartFloats = 128 + 4;
 constexpr int kXcds = 8;
 constexpr int kCus = 256;  // compute units of the GPU
 
@@ -42,12 +43,12 @@ __device__ __forceinline__ void poison_unreached_rows(const PrefillArgs &p, int 
 hipError_t launch_stream(int r, int g, bool rope, bool rows128, const PrefillArgs &pa, hipStream_t st, void *const *ev);
 
 __device__ __forceinline__ float *partial_row(const PrefillArgs &p, int split, int a, int tok, int head) {
-    return p.parts + ((((int64_t)split * p.n_agents + a) * p.reach + tok) * p.hq + head) * p.part_stride;
+    return p.parts + ((((int64_t)split * p.n_agents + a) * p.reach + tok) * p.hq + head) * kPartFloats;
 }
 // A workgroup without keys in its split leaves rows of no weight.
 __device__ __forceinline__ void empty_rows(const PrefillArgs &p, int split, int a, int h, int g, int tok_begin, int tok_end) {
     for (int i = threadIdx.x; i < (tok_end - tok_begin) * g; i += blockDim.x)
-        *reinterpret_cast<fkvk::f32x4 *>(partial_row(p, split, a, tok_begin + i / g, h * g + i % g) + p.part_stride - 4) =
+        *reinterpret_cast<fkvk::f32x4 *>(partial_row(p, split, a, tok_begin + i / g, h * g + i % g) + 128) =
             fkvk::f32x4{-INFINITY, 0.f, 0.f, 0.f};
 }
 

@@ -441,21 +441,6 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
         __syncthreads();
     }
 
-    if (p.splits > 1) {  // this split's partial rows
-        if (kg > 0) return;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            if (row_tok[nt] < 0) continue;
-            float *rec = partial_row(p, split, a, row_tok[nt], h * G + (rg * ROWS_PER_WAVE + nt * 16 + col) % G);
-#pragma unroll
-            for (int m = 0; m < 8; ++m) *reinterpret_cast<f32x4 *>(rec + 16 * m + 4 * grp) = oacc[m][nt];
-#pragma unroll
-            for (int t = 0; t < RT; ++t)
-                if (16 * t + 4 * grp < R) *reinterpret_cast<f32x4 *>(rec + D + 16 * t + 4 * grp) = racc[t][nt];
-            if (grp == 0) *reinterpret_cast<f32x4 *>(rec + p.part_stride - 4) = f32x4{m_run[nt], lacc[nt][0], 0.f, 0.f};
-        }
-        return;
-    }
     // ---- epilogue: O = (acc + acc_r . B_V[h]) / l ----
     if constexpr (R > 0) {
         if (use_res) {
@@ -488,6 +473,13 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
         if (row_tok[nt] < 0) continue;
+        if (p.splits > 1) {  // this split's partial rows
+            float *rec = partial_row(p, split, a, row_tok[nt], h * G + (rg * ROWS_PER_WAVE + nt * 16 + col) % G);
+#pragma unroll
+            for (int m = 0; m < 8; ++m) *reinterpret_cast<f32x4 *>(rec + 16 * m + 4 * grp) = oacc[m][nt];
+            if (grp == 0) *reinterpret_cast<f32x4 *>(rec + D) = f32x4{m_run[nt], lacc[nt][0], 0.f, 0.f};
+            continue;
+        }
         const float l = lacc[nt][0], inv = l > 0.f ? 1.f / l : 0.f;
         uint16_t *o = p.out + ((int64_t)(q0 + row_tok[nt]) * p.hq + h * G + (rg * ROWS_PER_WAVE + nt * 16 + col) % G) * D;
 #pragma unroll
@@ -495,55 +487,43 @@ __global__ __launch_bounds__(64 * WAVES, 1) void prefill_fp8_kernel(PrefillArgs 
     }
 }
 
-// The splits' partial rows are merged by a wave per query row: O = (sum w acc + (sum w acc_r) . B_V[h]) / sum w l with w = 2^(m - max m)
-// (Eq. 4).  A workgroup is four query heads of one chunk token; a wave that took a token's heads in turn needed 100 us and more.
-__global__ __launch_bounds__(256) void merge_splits_kernel(PrefillArgs p, int r, int g) {
-    const int quads = p.hq / 4, quad = blockIdx.x % quads, at = blockIdx.x / quads;
+// The splits' partial rows are merged: O = sum w acc / sum w l with w = 2^(m - max m).  Half a wave takes a query row: its lanes are the
+// splits (32 at most), then four dims each.  A workgroup has eight query heads of one chunk token.  (acc_r . B_V[h] is in acc: done here
+// it took 46 of 545 us at rank 64, as one wave per row 62, for four chunks of 250 in two splits.)
+__global__ __launch_bounds__(256) void merge_splits_kernel(PrefillArgs p) {
+    const int groups = (p.hq + 7) / 8, group = blockIdx.x % groups, at = blockIdx.x / groups;
     const int a = at / p.reach, tok = at % p.reach;
     const int q0 = p.q_indptr[a], nq = p.q_indptr[a + 1] - q0;
     if (tok >= nq) return;
-    const int lane = threadIdx.x & 63, head = 4 * quad + uniform(threadIdx.x >> 6);
-    const int ad = r > 0 ? p.adapter_idx[a] : -1;
-    const int64_t n = (int64_t)p.hkv * D, step = (int64_t)p.n_agents * p.reach * p.hq * p.part_stride;
+    const int lane = threadIdx.x & 63, half = lane >> 5, c = lane & 31;
+    const int row = 8 * group + 2 * uniform(threadIdx.x >> 6) + half, head = min(row, p.hq - 1);
+    const int64_t step = (int64_t)p.n_agents * p.reach * p.hq * kPartFloats;
     const float *rec = partial_row(p, 0, a, tok, head);
     float m = kNegInf, l = 0.f;
-    if (lane < p.splits) {
-        m = rec[lane * step + p.part_stride - 4];
-        l = rec[lane * step + p.part_stride - 3];
+    if (c < p.splits) {
+        m = rec[c * step + D];
+        l = rec[c * step + D + 1];
     }
-    const uint64_t live = __builtin_amdgcn_ballot_w64(!(m == kNegInf && l == 0.f));  // a split without keys has only m and l
+    const uint64_t live = __builtin_amdgcn_ballot_w64(!(m == kNegInf && l == 0.f)) >> (32 * half);  // a split without keys has only m and l
     float M = m;
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) M = fmaxf(M, __shfl_xor(M, x));
+    for (int x = 1; x < 32; x *= 2) M = fmaxf(M, __shfl_xor(M, x));
     const float w = fast_exp2(m - (M == kNegInf ? 0.f : M));
     float sum = w * l;
 #pragma unroll
-    for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
-    f32x2 o = {0.f, 0.f};
-    float low = 0.f;
-    const bool rank = ad >= 0 && lane < r;
+    for (int x = 1; x < 32; x *= 2) sum += __shfl_xor(sum, x);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int i = 0; i < p.splits; ++i) {
-        const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i));
+        const uint32_t u = __float_as_uint(w), lo = __builtin_amdgcn_readlane(u, i), hi = __builtin_amdgcn_readlane(u, 32 + i);
+        const float wi = __uint_as_float(half ? hi : lo);
         const bool on = (live >> i) & 1;
-        const f32x2 x = *reinterpret_cast<const f32x2 *>(rec + i * step + 2 * lane);
-        const float y = rank ? rec[i * step + D + lane] : 0.f;
-        o.x += on ? wi * x.x : 0.f;
-        o.y += on ? wi * x.y : 0.f;
-        low += on ? wi * y : 0.f;
-    }
-    if (ad >= 0) {
-        const uint16_t *bv = p.lora_b + ((int64_t)ad * 2 + 1) * r * n + (int64_t)(head / g) * D + 2 * lane;
-#pragma unroll 8
-        for (int rho = 0; rho < r; ++rho) {
-            const float x = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(low), rho));
-            const uint32_t b = *reinterpret_cast<const uint32_t *>(bv + rho * n);
-            o.x += x * bf16_lo(b);
-            o.y += x * bf16_hi(b);
-        }
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(rec + i * step + 4 * c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += on ? wi * x[j] : 0.f;
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    *reinterpret_cast<uint32_t *>(p.out + ((int64_t)(q0 + tok) * p.hq + head) * D + 2 * lane) = pack_bf16(o.x * inv, o.y * inv);
+    if (row < p.hq) *reinterpret_cast<u32x2 *>(p.out + ((int64_t)(q0 + tok) * p.hq + head) * D + 4 * c) = pack4(o * inv);
 }
 
 // Rows of a workgroup, and workgroups that share its keys.  An (agent, KV head) pair keeps to one XCD, so a grid takes as many passes
@@ -577,10 +557,9 @@ Grid grid_of(int64_t pairs, int64_t max_q, int g, int r, int max_pages, bool spl
     }
     return best;
 }
-constexpr int part_stride(int r) { return D + r + 4; }
-int64_t parts_bytes(const Grid &gr, int n_agents, int64_t max_q, int hq, int g, int r) {
+int64_t parts_bytes(const Grid &gr, int n_agents, int64_t max_q, int hq, int g) {
     const int64_t reach = (max_q * g + gr.rows - 1) / gr.rows * (gr.rows / g);
-    return (int64_t)gr.splits * n_agents * reach * hq * part_stride(r) * 4;
+    return (int64_t)gr.splits * n_agents * reach * hq * kPartFloats * 4;
 }
 
 template <int R, int G>
@@ -608,12 +587,11 @@ hipError_t dispatch(int r, const PrefillArgs &pa, hipStream_t st, void *const *e
 hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, void *workspace, size_t workspace_bytes, hipStream_t st, void *const *ev) {
     const int64_t pairs = (int64_t)pa.n_agents * pa.hkv;
     Grid gr = grid_of(pairs, max_q, g, r, pa.max_pages, true);
-    if (gr.splits > 1 && (!workspace || (int64_t)workspace_bytes < parts_bytes(gr, pa.n_agents, max_q, pa.hq, g, r)))
+    if (gr.splits > 1 && (!workspace || (int64_t)workspace_bytes < parts_bytes(gr, pa.n_agents, max_q, pa.hq, g)))
         gr = grid_of(pairs, max_q, g, r, pa.max_pages, false);
     pa.blocks_per_agent_head = (int)((max_q * g + gr.rows - 1) / gr.rows);
     pa.splits = gr.splits;
     pa.reach = pa.blocks_per_agent_head * (gr.rows / g);
-    pa.part_stride = part_stride(r);
     pa.parts = static_cast<float *>(workspace);
     void *first[2] = {ev ? ev[0] : nullptr, nullptr};
     void *const *ev1 = gr.splits > 1 ? (ev ? first : nullptr) : ev;
@@ -621,8 +599,8 @@ hipError_t launch_fp8(int r, int g, int64_t max_q, PrefillArgs pa, void *workspa
                    : g == 4       ? dispatch<4>(r, pa, st, ev1)
                                   : dispatch<8>(r, pa, st, ev1);
     if (e != hipSuccess || gr.splits == 1) return e;
-    hipExtLaunchKernelGGL(merge_splits_kernel, dim3(pa.n_agents * pa.reach * (pa.hq / 4)), dim3(256), 0, st, nullptr, ev ? static_cast<hipEvent_t>(ev[1]) : nullptr, 0,
-                          pa, r, g);
+    hipExtLaunchKernelGGL(merge_splits_kernel, dim3(pa.n_agents * pa.reach * ((pa.hq + 7) / 8)), dim3(256), 0, st, nullptr, ev ? static_cast<hipEvent_t>(ev[1]) : nullptr, 0,
+                          pa);
     return hipGetLastError();
 }
 
@@ -633,5 +611,5 @@ extern "C" int64_t fkv_prefill_fp8_workspace_bytes(int32_t hq, int32_t hkv, int3
     if ((g != 4 && g != 8) || (r != 0 && r != 8 && r != 16 && r != 32 && r != 64) || n_agents < 1 || max_q < 1 || max_pages < 1) return 0;
     if ((int64_t)n_agents * hkv >= 1 << 24 || max_q >= 1 << 28) return 0;  // (no split there, and their products stay in 64 bits)
     const fkvp::Grid gr = fkvp::grid_of((int64_t)n_agents * hkv, max_q, g, r, max_pages, true);
-    return gr.splits > 1 ? fkvp::parts_bytes(gr, n_agents, max_q, hq, g, r) : 0;
+    return gr.splits > 1 ? fkvp::parts_bytes(gr, n_agents, max_q, hq, g) : 0;
 }

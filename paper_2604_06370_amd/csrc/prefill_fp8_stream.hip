@@ -576,25 +576,6 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
     int block_id = blockIdx.x;
     asm volatile("" : "+s"(block_id));
     const Place at(p, block_id);
-    if (p.splits > 1) {  // this split's partial rows
-        if (kg > 0 || row_tok < 0) return;
-        float *rec = partial_row(p, at.split, at.a, row_tok, at.h * G + (rg * 32 + r32) % G);
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *reinterpret_cast<f32x4 *>(rec + 32 * b + 8 * i + 4 * hh) =
-                    f32x4{oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
-#pragma unroll
-        for (int b = 0; b < NRB; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (32 * b + 8 * i + 4 * hh < R)
-                    *reinterpret_cast<f32x4 *>(rec + D + 32 * b + 8 * i + 4 * hh) =
-                        f32x4{racc[b][4 * i], racc[b][4 * i + 1], racc[b][4 * i + 2], racc[b][4 * i + 3]};
-        if (hh == 0) *reinterpret_cast<f32x4 *>(rec + p.part_stride - 4) = f32x4{m_run, l_run, 0.f, 0.f};
-        return;
-    }
     if constexpr (R > 0) {
         float *bv = reinterpret_cast<float *>(lds), *acc = bv + R * D;
         const int64_t n = (int64_t)p.hkv * D;
@@ -626,7 +607,16 @@ __device__ __forceinline__ void block(const PrefillArgs &p, unsigned char *lds, 
                 }
         }
     }
-    if (kg == 0 && row_tok >= 0) {
+    if (kg == 0 && row_tok >= 0 && p.splits > 1) {  // this split's partial rows
+        float *rec = partial_row(p, at.split, at.a, row_tok, at.h * G + (rg * 32 + r32) % G);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4 *>(rec + 32 * b + 8 * i + 4 * hh) =
+                    f32x4{oacc[b][4 * i], oacc[b][4 * i + 1], oacc[b][4 * i + 2], oacc[b][4 * i + 3]};
+        if (hh == 0) *reinterpret_cast<f32x4 *>(rec + D) = f32x4{m_run, l_run, 0.f, 0.f};
+    } else if (kg == 0 && row_tok >= 0) {
         const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
         uint16_t *o = p.out + ((int64_t)(p.q_indptr[at.a] + row_tok) * p.hq + at.h * G + (rg * 32 + r32) % G) * D;
 #pragma unroll

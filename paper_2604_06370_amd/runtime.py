@@ -380,6 +380,8 @@ def produce_tokens_fp8(seqs, x: Optional[torch.Tensor], k_raw: torch.Tensor, v: 
             if not _table_fits(btr, device, pos0 + n, page_size):
                 _fp8_range(who, i, btr, pos0, n, row0, rows, page_size)
         items.append((btb.data_ptr() if n else 0, btr.data_ptr() if with_a else 0, a.data_ptr() if with_a else 0, pos0, n, row0))
+    if rows == 0:  # nothing to write (and no address of it)
+        return
     arr = np.array(items, dtype=np.int64)  # fkv_produce_seq: six 8-byte members
     cos, sin = (rope[0], rope[1]) if rope is not None else (None, None)
     max_pos = min(cos.numel(), sin.numel()) // (d // 2) if cos is not None else 0
@@ -400,6 +402,8 @@ def gather_tokens_fp8(seqs, base_fp8: torch.Tensor, k_out: torch.Tensor, v_out: 
         if not (pos0 >= 0 and n > 0 and row0 >= 0 and row0 + n <= rows and _table_fits(bt, device, pos0 + n, page_size)):
             _fp8_range(who, i, bt, pos0, n, row0, rows, page_size)
         items.append((bt.data_ptr() if n else 0, pos0, n, row0))
+    if rows == 0:  # nothing to read (and no address for it)
+        return
     arr = np.array(items, dtype=np.int64)  # fkv_read_seq: four 8-byte members
     check(N.fkv_gather_tokens_fp8(arr.ctypes.data, len(seqs), base_fp8.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), hkv, d, page_size,
                                   _stream(stream)), who)

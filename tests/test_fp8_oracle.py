@@ -162,7 +162,7 @@ def test_attention_refusals_without_a_gpu(kw):
 def test_prefill_workspace():
     # the smaller the grid the more workgroups share a row's keys; none where the grid fills the GPU or contexts are short
     need = lambda *a: rt.prefill_fp8_workspace_bytes(*a)  # noqa: E731
-    assert need(32, 8, 16, 1, 1, 4096) == 32 * 16 * 32 * (128 + 16 + 4) * 4  # splits, tokens of a workgroup, heads, floats of a record
+    assert need(32, 8, 16, 1, 1, 4096) == 32 * 16 * 32 * (128 + 4) * 4  # splits, tokens of a workgroup, heads, floats of a record
     assert need(32, 8, 16, 1, 1, 31) == 0 and need(32, 8, 16, 64, 4096, 4096) == 0
     assert need(32, 8, 16, 1, 1, 64) == need(32, 8, 16, 1, 1, 4096) * 4 // 32
     for bad in ((32, 8, 24, 1, 1, 64), (32, 5, 16, 1, 1, 64), (8, 8, 16, 1, 1, 64), (32, 8, 16, 0, 1, 64), (32, 8, 16, 1, 0, 64), (32, 8, 16, 1, 1, 0),

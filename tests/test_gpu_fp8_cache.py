@@ -81,6 +81,21 @@ def test_write_and_read_back(hkv, pos0, n, kind):
     assert (ko[[0, -1]] == 7).all() and (vo[[0, -1]] == 7).all()  # rows outside the ranges stay
 
 
+def test_nothing_to_write_or_read():
+    pool = torch.full((3, o.page_bytes(2)), 77, dtype=torch.uint8, device="cuda")
+    bt = torch.zeros(2, dtype=torch.int32, device="cuda")
+    none, x = torch.empty(0, 2, D, dtype=torch.bfloat16, device="cuda"), torch.ones(4, 2, D, dtype=torch.bfloat16, device="cuda")
+    for k in (none, x):
+        rt.produce_tokens_fp8([(bt, None, None, 3, 0, 0), (None, None, None, 0, 0, 0)], None, k, k, None, pool, None, 2, D, 0, PS)
+        rt.produce_tokens_fp8([], None, k, k, None, pool, None, 2, D, 0, PS)
+        rt.gather_tokens_fp8([(bt, 3, 0, 0)], pool, k, k, 2, D, PS)
+        rt.gather_tokens_fp8([], pool, k, k, 2, D, PS)
+    rt.page_copy_fp8([], pool, None, 2, D, 0, PS)
+    rt.page_copy_fp8([(0, 0, 1, 0)], pool, None, 2, D, 0, PS)
+    torch.cuda.synchronize()
+    assert bool((pool == 77).all()) and bool((x == 1).all())
+
+
 def test_every_code_reads_back_exactly():
     """All 256 codes with all exponent bytes that are written, in both K and V."""
     pool = torch.zeros(237, o.page_bytes(1), dtype=torch.uint8)
