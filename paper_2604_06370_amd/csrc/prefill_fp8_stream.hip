@@ -17,7 +17,7 @@
 // end of its step, when the products of the step before, which carry the old one, are in.
 //
 // Measured at 16 chunks of 1024 tokens over 9.5k tokens of context, 8B heads: 950 TFLOP/s without adapters (a large bf16 product of
-// the library: 1140), 905 with rank 16 (prefill_fp8.hip's kernel at 256 rows: 823), 757 with RoPE (712), and 700 at rank 64 with RoPE
+// the library: 1140), 905 with rank 16 (prefill_fp8.hip's kernel at 256 rows: 823), 757 with RoPE (712), and 727 at rank 64 with RoPE
 // over 70B heads (511).
 //
 // Where 256 rows leave compute units idle a workgroup has 128 rows in four row groups, and two key groups of four waves take one half
