@@ -334,6 +334,25 @@ def test_prefill_splits_in_a_graph_and_on_two_streams():
         assert torch.equal(eager, want[0]) and all(torch.equal(out, w) for out, w in zip(outs, want))
 
 
+def test_prefill_splits_on_a_forked_stream_of_a_graph():
+    p = Problem(22, [6000, 70], 0, 32, 8, 16, True, rows=[5, 9])
+    want, out = p.prefill(), torch.zeros_like(p.q)
+    args = p.args(out, q_indptr=p.indptr, n_q=14, max_q_per_agent=9)
+    assert rt.prefill_fp8_workspace_bytes(32, 8, 16, 2, 9, p.base.shape[1]) > 0
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        rt.residual_attention_prefill_fp8(args, side)
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(4):
+        out.zero_()
+        graph.replay()
+        eager = p.prefill()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(eager, want)
+
+
 @pytest.mark.parametrize("raw", [False, True])
 def test_prefill_scratch_belongs_to_its_stream(raw):
     """Memory freed on the current stream with work pending there is not the scratch of a call on another stream."""
