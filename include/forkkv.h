@@ -484,6 +484,7 @@ fkv_status fkv_residual_attention_prefill_fp8(const fkv_attn_args *args, void *s
 /* Prefill of few query rows over long contexts splits their keys over workgroups, whose partial rows (fp32) are merged by a second
  * kernel: where args->workspace (16-byte aligned) has these bytes for the sizes of args (max_q: its max_q_per_agent, or n_q).
  * With less, or none, one workgroup passes over all keys of a row.  0: that is the way for these sizes, or they are not taken.
+ * max_pages stands for the contexts' length: tables much wider than the contexts split short ones too, at about 10 us.
  * Calls that share a workspace must not overlap. */
 int64_t fkv_prefill_fp8_workspace_bytes(int32_t hq, int32_t hkv, int32_t r, int32_t n_agents, int32_t max_q, int32_t max_pages);
 
